@@ -154,6 +154,19 @@ extern "C" {
 #define BSR_STRUCT_DEV_STATUS 4
 #define BSR_STRUCT_STATS 5
 #define BSR_STRUCT_ADMISSION 6
+#define BSR_STRUCT_TABLE_GROUP 7
+#define BSR_STRUCT_TABLES_ARGS 8
+#define BSR_STRUCT_APPEND_ARGS 9
+#define BSR_STRUCT_ATTN_ARGS 10
+
+/* value types of the paged cache's operators */
+#define BSR_TYPE_BF16 0
+#define BSR_TYPE_F16 1
+#define BSR_TYPE_F32 2         /* a source of bsr_cache_append only */
+#define BSR_TYPE_E4M3_SCALED 3 /* PLANAR records of fp8-e4m3fn values and their fp32 scale */
+
+#define BSR_MAX_TABLE_REQUESTS 4096 /* requests of one bsr_tables_build */
+#define BSR_MAX_TREE_WORDS 16       /* 64-bit words of one node's tree mask: up to 1,024 nodes a request */
 
 typedef struct bsr_group_desc {
   uint32_t block_tokens; /* tokens per destination block, >= 1 */
@@ -557,6 +570,156 @@ int bsr_direct_stats(bsr_ctx* ctx, uint64_t request_id, uint32_t* n_launches, ui
 
 /* Admission state: B, session slots, what is bound now and the peaks. */
 int bsr_admission_get(bsr_ctx* ctx, bsr_admission* out);
+
+/* ---- the paged cache around a restore --------------------------------------------
+ *
+ * What an engine runs on the blocks that a restore fills: it lays them out
+ * (bsr_tables_build, whose tables bind and commit take), writes the new
+ * tokens' records behind the restored prefix (bsr_cache_append), and reads
+ * the cache with their queries (bsr_attend_tree, bsr_attend_prompt).
+ *
+ *   - The context gives the device and the layout (a group's block_tokens,
+ *     record_bytes, kind and split_bytes); it needs a GPU (BSR_E_DEVICE) and
+ *     keeps nothing from one call for the next.  Calls take no lock.
+ *   - Every call is asynchronous on `stream`, allocates nothing, reads no
+ *     device memory on the host and may be captured into a graph; the
+ *     lengths are read on the device, so a replay follows their new values.
+ *     The caller's current device is left as it was.
+ *   - The args structs and the host arrays they point to are read before the
+ *     call returns.  Unless said otherwise pointers in them are device
+ *     pointers, and outputs overlap neither inputs nor one another.
+ *   - Two calls that may run at once need workspaces of their own.
+ *   - Refused arguments return BSR_E_ARG and enqueue nothing.  Device
+ *     contents are checked on the device: block ids outside the pool and
+ *     slots outside it are neither read nor written.
+ */
+
+/* One group's blocks for bsr_tables_build. */
+typedef struct bsr_table_group {
+  const int32_t* free_blocks; /* int32[n_free]: ids of free blocks, taken from the front; no id twice */
+  int32_t* tables;            /* int32[n_requests][table_stride]: in, each request's held blocks; out, the
+                                 blocks it takes behind them.  NULL leaves the group out (then slots must be
+                                 NULL too) */
+  int64_t* slots;             /* int64[n_slots]: out, slot of every new token; may be NULL */
+  uint32_t n_free;
+  uint32_t table_stride;      /* entries of one request's table */
+} bsr_table_group;
+
+typedef struct bsr_tables_args {
+  uint32_t n_requests;     /* 0..BSR_MAX_TABLE_REQUESTS */
+  uint32_t n_slots;        /* rows that the batch has room for, < 2^31 */
+  const int32_t* cached;   /* int32[n_requests]: tokens that each request holds */
+  const int32_t* added;    /* int32[n_requests]: tokens that it gets */
+  int32_t* starts;         /* int32[n_requests + 1]: out, its first row among the new tokens, and their number */
+  int32_t* lens;           /* int32[n_requests]: out, the tokens that it holds then */
+  uint32_t* result;        /* uint32[1 + n_groups]: out, requests admitted, then blocks taken per group */
+  const bsr_table_group* groups; /* host array, one per group of the context's layout */
+} bsr_tables_args;
+
+/* Block tables and slot maps of a batch from its requests' lengths, all
+ * groups in one launch.  With B = block_tokens, request r holds
+ * ceil(cached/B) blocks of a group and takes ceil((cached+added)/B) less
+ * those, from the front of free_blocks, in the order of the requests; its new
+ * tokens are rows starts[r] .. starts[r+1]-1 of the batch, and token t's slot
+ * is tables[r][t / B] * B + t % B (-1 behind the last row, and where the block
+ * id is negative).  Requests are admitted in order, each whole or not at all:
+ * the first whose blocks are not all there in every group, whose table or rows
+ * have no room, or whose lengths are negative or sum to 2^31 or more, and every
+ * one after it, gets nothing (no rows, lens = cached, at least 0).  Entries of
+ * the tables other than the taken ones are left as they are.  BSR_E_ARG also
+ * where lens or starts overlap cached or added. */
+int bsr_tables_build(bsr_ctx* ctx, const bsr_tables_args* args, void* stream);
+
+typedef struct bsr_append_args {
+  uint32_t group;        /* of the context's layout */
+  uint32_t n_tokens;     /* rows; 0 does nothing */
+  const int64_t* slots;  /* int64[n_tokens]: block * block_tokens + position; rows whose slot lies outside
+                            [0, pool_blocks * block_tokens) are skipped.  No slot twice */
+  void* pool;            /* one tensor's pool, 16-byte aligned */
+  uint32_t pool_blocks;
+  uint32_t src_type;     /* BSR_TYPE_BF16, F16 or F32 */
+  uint32_t cache_type;   /* CONTIG: BSR_TYPE_BF16 or F16; PLANAR: BSR_TYPE_E4M3_SCALED */
+  uint32_t n_sources;    /* 1 or 2: a record is a row of the first, then one of the second */
+  const void* src[2];    /* [n_tokens][width] values, aligned to their type */
+  uint32_t width[2];     /* values of a row; together the record's (PLANAR: split_bytes) */
+  int64_t src_stride[2]; /* values from one row to the next, >= width */
+} bsr_append_args;
+
+/* New tokens' records into their slots of one tensor.  CONTIG: each value
+ * rounded to nearest even to cache_type (same type: copied).  PLANAR, of
+ * record_bytes = split_bytes + 4: scale = max|x| / 448 in fp32, values
+ * x / scale rounded to nearest even to fp8-e4m3fn; a record whose scale is zero has zeros, and one
+ * with an infinity or a NaN a scale of NaN and zeros, so that all of it reads
+ * back as NaN. */
+int bsr_cache_append(bsr_ctx* ctx, const bsr_append_args* args, void* stream);
+
+/* Attention over the paged cache.  Request r's queries are rows
+ * starts[r] .. starts[r+1]-1 of q, its last tokens: with n = lens[r] tokens in
+ * the cache, theirs included (append them first), and T rows, row i stands at
+ * n - T + i.  Query head h reads KV head h / (n_heads / n_kv_heads). */
+typedef struct bsr_attn_args {
+  uint32_t group;       /* of the context's layout: CONTIG, record_bytes a multiple of 16 */
+  uint32_t dtype;       /* of q, out and the cache: BSR_TYPE_BF16 or F16 */
+  uint32_t n_requests;  /* 0 does nothing */
+  uint32_t n_tokens;    /* rows of q, out, lse; those at starts[n_requests] and after stay as they are */
+  uint32_t n_heads;     /* a multiple of n_kv_heads */
+  uint32_t n_kv_heads;
+  uint32_t k_dim, v_dim; /* (64, 64), (128, 128), or (576, 512): latent records, one KV head, whose value is
+                            the first 512 of the key (v_pool = k_pool, v_offset = k_offset) */
+  const void* q;         /* [n_tokens][n_heads][k_dim], 16-byte aligned; strides in values, multiples of 8,
+                            the last dimension contiguous */
+  int64_t q_token_stride, q_head_stride;
+  void* out;             /* [n_tokens][n_heads][v_dim], likewise */
+  int64_t out_token_stride, out_head_stride;
+  float* lse;            /* fp32 [n_tokens][n_heads]: natural logarithm of the sum of exp(score); may be NULL */
+  const void* k_pool;    /* pools of pool_blocks blocks, 16-byte aligned; KV head g of a token lies at */
+  const void* v_pool;    /* k_offset + g * 2 * k_dim (v_offset + g * 2 * v_dim) bytes of its record */
+  uint32_t k_offset, v_offset; /* multiples of 16 */
+  uint32_t pool_blocks;
+  uint32_t table_stride;       /* entries of one request's block table */
+  const int32_t* tables;       /* int32[n_requests][table_stride] */
+  const int32_t* starts;       /* int32[n_requests + 1], not decreasing */
+  const int32_t* lens;         /* int32[n_requests], at most max_len and what the table holds (taken as that
+                                  where they are more) */
+  uint32_t max_len;            /* bound of lens that the host knows, < 2^31 */
+  uint32_t window;             /* 0, or how many keys up to its own position a row sees at most */
+  float scale;                 /* > 0 */
+  float softcap;               /* 0, or c > 0: the score is c * tanh(scale * q.k / c) */
+  void* workspace;             /* bsr_attn_workspace_bytes, 16-byte aligned; contents need not be kept */
+  uint64_t workspace_bytes;
+  /* bsr_attend_tree */
+  const uint64_t* tree;  /* uint64[n_tokens][tree_words]: bit k of row i is set where row i of the request sees
+                            row k of it */
+  uint32_t tree_words;   /* 1..BSR_MAX_TREE_WORDS; rows past 64 * tree_words are seen by none */
+  uint32_t reserved;     /* 0 */
+  /* bsr_attend_prompt; each may be NULL */
+  const float* slopes;      /* fp32[n_heads]: the score less slope * |distance of the positions| */
+  const int32_t* prefix;    /* int32[n_requests]: keys before it are seen by every row (bidirectional prefix) */
+  const int32_t* documents; /* int32[n_tokens]: first position of the row's document; keys before it are not seen */
+} bsr_attn_args;
+
+/* Workspace bytes of either call for these arguments (the sizes, types and
+ * layout alone count); 0 if none is needed, BSR_ATTN_REFUSED on refused arguments. */
+#define BSR_ATTN_REFUSED UINT64_MAX
+uint64_t bsr_attn_workspace_bytes(bsr_ctx* ctx, const bsr_attn_args* args);
+
+/* Attention for a tree of drafted tokens, or for single tokens (a tree of one
+ * node that sees itself).  Row i sees every token before its request's rows, and
+ * the rows whose bits its mask has.  window: a row stands at n - T + (its bits set) - 1,
+ * and sees no token before the rows that is `window` or more positions back; a
+ * window smaller than 64 * tree_words, where the tree itself could outgrow it,
+ * is refused.  slopes, prefix and documents must be NULL.
+ *
+ * Here and below: sums, the softmax and lse are in fp32, the weights are
+ * rounded to dtype for the products with the values, and out is rounded once.
+ * A row that sees no key gets zeros and lse = -infinity.  Keys that a row does not
+ * see count for nothing, whatever they hold, infinities and NaN included.  Blocks whose id lies
+ * outside [0, pool_blocks) are not read and not seen. */
+int bsr_attend_tree(bsr_ctx* ctx, const bsr_attn_args* args, void* stream);
+
+/* Attention of prompt tokens.  With p = n - T + i, row i sees keys j with
+ * j <= p or j < min(prefix, n), j > p - window if there is one, and j >= documents[row].  tree must be NULL. */
+int bsr_attend_prompt(bsr_ctx* ctx, const bsr_attn_args* args, void* stream);
 
 /* ---- instrumentation ----------------------------------------------------------- */
 

@@ -39,7 +39,13 @@ BSR_INJECT_NONE, BSR_INJECT_DELAY_MS, BSR_INJECT_TRANSFER_ERROR, BSR_INJECT_LAUN
 BSR_TIER_PINNED, BSR_TIER_FILE, BSR_TIER_NONE = 0, 1, 255
 BSR_FILE_DIRECT = 1
 
-_STRUCT_IDS = {"layout": 1, "config": 2, "group_dst": 3, "dev_status": 4, "stats": 5, "admission": 6}
+BSR_TYPE_BF16, BSR_TYPE_F16, BSR_TYPE_F32, BSR_TYPE_E4M3_SCALED = 0, 1, 2, 3
+BSR_MAX_TABLE_REQUESTS = 4096
+BSR_MAX_TREE_WORDS = 16
+BSR_ATTN_REFUSED = (1 << 64) - 1
+
+_STRUCT_IDS = {"layout": 1, "config": 2, "group_dst": 3, "dev_status": 4, "stats": 5, "admission": 6,
+               "table_group": 7, "tables_args": 8, "append_args": 9, "attn_args": 10}
 
 
 class bsr_group_desc(ct.Structure):
@@ -92,6 +98,39 @@ class bsr_admission(ct.Structure):
                 ("n_bound", ct.c_uint32), ("bound_staging_bytes", ct.c_uint64),
                 ("peak_bound_staging_bytes", ct.c_uint64), ("peak_n_bound", ct.c_uint32),
                 ("n_refused", ct.c_uint32), ("aux_device_bytes", ct.c_uint64)]
+
+
+class bsr_table_group(ct.Structure):
+    _fields_ = [("free_blocks", ct.c_void_p), ("tables", ct.c_void_p), ("slots", ct.c_void_p),
+                ("n_free", ct.c_uint32), ("table_stride", ct.c_uint32)]
+
+
+class bsr_tables_args(ct.Structure):
+    _fields_ = [("n_requests", ct.c_uint32), ("n_slots", ct.c_uint32), ("cached", ct.c_void_p),
+                ("added", ct.c_void_p), ("starts", ct.c_void_p), ("lens", ct.c_void_p), ("result", ct.c_void_p),
+                ("groups", ct.POINTER(bsr_table_group))]
+
+
+class bsr_append_args(ct.Structure):
+    _fields_ = [("group", ct.c_uint32), ("n_tokens", ct.c_uint32), ("slots", ct.c_void_p), ("pool", ct.c_void_p),
+                ("pool_blocks", ct.c_uint32), ("src_type", ct.c_uint32), ("cache_type", ct.c_uint32),
+                ("n_sources", ct.c_uint32), ("src", ct.c_void_p * 2), ("width", ct.c_uint32 * 2),
+                ("src_stride", ct.c_int64 * 2)]
+
+
+class bsr_attn_args(ct.Structure):
+    _fields_ = [("group", ct.c_uint32), ("dtype", ct.c_uint32), ("n_requests", ct.c_uint32),
+                ("n_tokens", ct.c_uint32), ("n_heads", ct.c_uint32), ("n_kv_heads", ct.c_uint32),
+                ("k_dim", ct.c_uint32), ("v_dim", ct.c_uint32), ("q", ct.c_void_p),
+                ("q_token_stride", ct.c_int64), ("q_head_stride", ct.c_int64), ("out", ct.c_void_p),
+                ("out_token_stride", ct.c_int64), ("out_head_stride", ct.c_int64), ("lse", ct.c_void_p),
+                ("k_pool", ct.c_void_p), ("v_pool", ct.c_void_p), ("k_offset", ct.c_uint32),
+                ("v_offset", ct.c_uint32), ("pool_blocks", ct.c_uint32), ("table_stride", ct.c_uint32),
+                ("tables", ct.c_void_p), ("starts", ct.c_void_p), ("lens", ct.c_void_p), ("max_len", ct.c_uint32),
+                ("window", ct.c_uint32), ("scale", ct.c_float), ("softcap", ct.c_float),
+                ("workspace", ct.c_void_p), ("workspace_bytes", ct.c_uint64), ("tree", ct.c_void_p),
+                ("tree_words", ct.c_uint32), ("reserved", ct.c_uint32), ("slopes", ct.c_void_p),
+                ("prefix", ct.c_void_p), ("documents", ct.c_void_p)]
 
 
 class BsrError(RuntimeError):
@@ -147,6 +186,11 @@ def _load() -> ct.CDLL:
         "bsr_file_tier_count": (ct.c_int, [VP, P(U64)]),
         "bsr_tier_set_available": (ct.c_int, [VP, I32, I32]),
         "bsr_plan_tiers": (ct.c_int, [VP, U64, VP, U32]),
+        "bsr_tables_build": (ct.c_int, [VP, P(bsr_tables_args), VP]),
+        "bsr_cache_append": (ct.c_int, [VP, P(bsr_append_args), VP]),
+        "bsr_attn_workspace_bytes": (U64, [VP, P(bsr_attn_args)]),
+        "bsr_attend_tree": (ct.c_int, [VP, P(bsr_attn_args), VP]),
+        "bsr_attend_prompt": (ct.c_int, [VP, P(bsr_attn_args), VP]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -154,7 +198,9 @@ def _load() -> ct.CDLL:
     if lib.bsr_abi_version() != BSR_ABI_VERSION:
         raise ImportError(f"libbsr.so ABI {lib.bsr_abi_version()} != binding ABI {BSR_ABI_VERSION}; rebuild")
     for name, cls in (("layout", bsr_layout), ("config", bsr_config), ("group_dst", bsr_group_dst),
-                      ("dev_status", bsr_dev_status), ("stats", bsr_stats), ("admission", bsr_admission)):
+                      ("dev_status", bsr_dev_status), ("stats", bsr_stats), ("admission", bsr_admission),
+                      ("table_group", bsr_table_group), ("tables_args", bsr_tables_args),
+                      ("append_args", bsr_append_args), ("attn_args", bsr_attn_args)):
         n = lib.bsr_struct_size(_STRUCT_IDS[name])
         if n != ct.sizeof(cls):
             raise ImportError(f"struct {name}: library size {n} != binding size {ct.sizeof(cls)}")
@@ -444,3 +490,60 @@ def bsr_plan_tiers(ctx: Ctx, request_id: int, n_chunks: int) -> np.ndarray:
     out = np.zeros(max(1, n_chunks), dtype=np.uint8)
     _check(_lib.bsr_plan_tiers(ctx, request_id, _ptr(out), n_chunks))
     return out[:n_chunks]
+
+
+# ---- the paged cache around a restore ----------------------------------------------
+# The args structs hold addresses: a program may fill one once and pass it call
+# after call while its buffers stay.
+def table_group(free_blocks_ptr: int, n_free: int, tables_ptr: int, table_stride: int,
+                slots_ptr: int = 0) -> bsr_table_group:
+    return bsr_table_group(free_blocks_ptr, tables_ptr, slots_ptr, n_free, table_stride)
+
+
+def tables_args(n_requests: int, cached_ptr: int, added_ptr: int, groups: Sequence[bsr_table_group], n_slots: int,
+                starts_ptr: int, lens_ptr: int, result_ptr: int) -> bsr_tables_args:
+    arr = (bsr_table_group * max(1, len(groups)))(*groups)
+    a = bsr_tables_args(n_requests, n_slots, cached_ptr, added_ptr, starts_ptr, lens_ptr, result_ptr, arr)
+    a.n_group_entries = len(groups)
+    return a
+
+
+def bsr_tables_build(ctx: Ctx, args: bsr_tables_args, stream: int) -> None:
+    if args.n_group_entries != ctx.layout.n_groups:
+        raise BsrError(BSR_E_ARG, f"{args.n_group_entries} table groups, the layout has {ctx.layout.n_groups}")
+    _check(_lib.bsr_tables_build(ctx, ct.byref(args), stream))
+
+
+def append_args(group: int, n_tokens: int, slots: int, pool: int, pool_blocks: int, src_type: int, cache_type: int,
+                sources: Sequence[Tuple[int, int, int]]) -> bsr_append_args:
+    """sources: (address, values of a row, values from one row to the next), one or two."""
+    a = bsr_append_args(group, n_tokens, slots, pool, pool_blocks, src_type, cache_type, len(sources))
+    for i, (addr, width, stride) in enumerate(sources[:2]):
+        a.src[i], a.width[i], a.src_stride[i] = addr, width, stride
+    return a
+
+
+def bsr_cache_append(ctx: Ctx, args: bsr_append_args, stream: int) -> None:
+    _check(_lib.bsr_cache_append(ctx, ct.byref(args), stream))
+
+
+def attn_args(q_strides: Tuple[int, int], out_strides: Tuple[int, int], **fields) -> bsr_attn_args:
+    """Fields of bsr_attn_args by name; strides are (token, head) in values."""
+    return bsr_attn_args(q_token_stride=q_strides[0], q_head_stride=q_strides[1],
+                         out_token_stride=out_strides[0], out_head_stride=out_strides[1], **fields)
+
+
+def bsr_attn_workspace_bytes(ctx: Ctx, args: bsr_attn_args) -> int:
+    """0 where none is needed; raises on refused arguments."""
+    n = _lib.bsr_attn_workspace_bytes(ctx, ct.byref(args))
+    if n == BSR_ATTN_REFUSED:
+        raise BsrError(BSR_E_ARG, bsr_last_error())
+    return n
+
+
+def bsr_attend_tree(ctx: Ctx, args: bsr_attn_args, stream: int) -> None:
+    _check(_lib.bsr_attend_tree(ctx, ct.byref(args), stream))
+
+
+def bsr_attend_prompt(ctx: Ctx, args: bsr_attn_args, stream: int) -> None:
+    _check(_lib.bsr_attend_prompt(ctx, ct.byref(args), stream))

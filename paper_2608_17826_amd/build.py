@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libbsr.so")
 
-SOURCES = ["bsr_kernels.hip", "bsr_runtime.cpp", "bsr_file_tier.cpp"]
+SOURCES = ["bsr_kernels.hip", "bsr_runtime.cpp", "bsr_file_tier.cpp", "bsr_cache.cpp", "bsr_cache.hip",
+           "bsr_attention.hip"]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}", "-Wall",
@@ -53,7 +54,7 @@ def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     objs = []
     for src in SOURCES:
-        obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
+        obj = os.path.join(BUILD, src + ".o")
         # a fixed compilation-unit id keeps the device code object independent
         # of where the tree is built (it is otherwise derived from the path)
         lang = ["-x", "hip", "-cuid=" + os.path.splitext(src)[0]] if src.endswith(".hip") else []

@@ -894,6 +894,16 @@ int host_fail(bsr_ctx* c, Session& s, int reason, uint32_t chunk, uint32_t mask,
 
 }  // namespace
 
+// What the paged cache's operators (bsr_cache.cpp) take from a context: its
+// layout and device, fixed when it is created, and the thread's error message.
+namespace bsr {
+
+const bsr_layout* ctx_layout(const bsr_ctx* c) { return &c->geo.L; }
+int ctx_device(const bsr_ctx* c) { return c->device; }
+int set_error(int code, const char* message) { return fail_with(code, "%s", message); }
+
+}  // namespace bsr
+
 // ===========================================================================
 // C ABI
 // ===========================================================================
@@ -909,6 +919,10 @@ uint64_t bsr_struct_size(int32_t which) {
     case BSR_STRUCT_DEV_STATUS: return sizeof(bsr_dev_status);
     case BSR_STRUCT_STATS: return sizeof(bsr_stats);
     case BSR_STRUCT_ADMISSION: return sizeof(bsr_admission);
+    case BSR_STRUCT_TABLE_GROUP: return sizeof(bsr_table_group);
+    case BSR_STRUCT_TABLES_ARGS: return sizeof(bsr_tables_args);
+    case BSR_STRUCT_APPEND_ARGS: return sizeof(bsr_append_args);
+    case BSR_STRUCT_ATTN_ARGS: return sizeof(bsr_attn_args);
     default: return 0;
   }
 }
