@@ -136,45 +136,898 @@ __device__ void attend_row(const AttnParams& p, const Request& q, const Row& w, 
   }
 }
 
-constexpr int kRowThreads = 256;
 
-// A wave per row and head.
-template <typename T, int KD, int VD>
-__global__ __launch_bounds__(kRowThreads) void k_attend_rows(AttnParams p) {
-  const uint32_t row = blockIdx.x, head = blockIdx.y * (kRowThreads / 64) + threadIdx.x / 64;
-  if (head >= p.n_heads || static_cast<int>(row) >= p.starts[p.n_requests]) return;
-  uint32_t lo = 0, hi = p.n_requests;  // the last request that starts at or before the row
-  while (hi - lo > 1) {
-    const uint32_t mid = (lo + hi) / 2;
-    if (p.starts[mid] <= static_cast<int>(row)) lo = mid;
-    else hi = mid;
+// ---------------------------------------------------------------------------
+// The work: a tile is kTileRows query rows, tile_tokens tokens times
+// tile_heads heads of one KV head, so that a key read once serves them all.
+// Where a batch has few tiles its key ranges are cut into parts, and a second
+// kernel joins them.  Every workgroup finds its item from the lengths alone:
+// nothing about them is known to the host.
+// ---------------------------------------------------------------------------
+struct Work {
+  uint32_t r;       // request
+  uint32_t tile;    // of the request's tokens
+  uint32_t unit;    // KV head x chunk of its heads
+  uint32_t split, n_splits;
+  uint32_t slot;    // first partial result of the item's parts
+};
+
+struct RequestWork {
+  uint32_t tiles, range;  // tiles of tokens, keys that one of them can see at most
+};
+
+__device__ __forceinline__ RequestWork request_work(const AttnParams& p, uint32_t r) {
+  RequestWork w{0, 0};
+  if (r >= p.n_requests) return w;
+  const Request q = request_of(p, r);
+  w.tiles = (q.rows + p.tile_tokens - 1) / p.tile_tokens;
+  w.range = q.n;
+  if (p.window && !p.prefix) w.range = min(w.range, p.window + (p.tree ? q.rows : min(static_cast<uint32_t>(q.rows), p.tile_tokens)));
+  return w;
+}
+
+__device__ __forceinline__ uint32_t splits_of(uint32_t range, uint32_t part) { return range > part ? (range + part - 1) / part : 1; }
+
+__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) {
+  const uint32_t lo = __shfl_up(static_cast<uint32_t>(v), d), hi = __shfl_up(static_cast<uint32_t>(v >> 32), d);
+  return static_cast<uint64_t>(hi) << 32 | lo;
+}
+__device__ __forceinline__ uint64_t shfl64(uint64_t v, int l) {
+  const uint32_t lo = __shfl(static_cast<uint32_t>(v), l), hi = __shfl(static_cast<uint32_t>(v >> 32), l);
+  return static_cast<uint64_t>(hi) << 32 | lo;
+}
+
+// Keys of a part: the batch's (tile, key) pairs over the target, so that the
+// parts come out alike whatever the requests' lengths.  Parts of ranges that are cut
+// at all number at most 2 x target (each range is longer than a part).
+__device__ __forceinline__ uint32_t part_keys(const AttnParams& p) {
+  if (!p.target) return 0x7fffffffu;
+  const uint32_t lane = threadIdx.x & 63;
+  uint64_t total = 0;
+  for (uint32_t r0 = 0; r0 < p.n_requests; r0 += 64) {
+    const RequestWork w = request_work(p, r0 + lane);
+    total += static_cast<uint64_t>(w.tiles) * w.range;
   }
-  const Request q = request_of(p, lo);
-  const int i = static_cast<int>(row) - q.first;
-  if (i < 0 || i >= q.rows) return;
-  const Row w = row_of(p, q, lo, i);
-  float m, l, acc[VD / 64];
-  attend_row<T, KD, VD>(p, q, w, i, head, max(w.lo, 0), min(w.hi, q.n), m, l, acc);
-  T* o = reinterpret_cast<T*>(p.out + row * p.out_token + head * p.out_head) + (threadIdx.x & 63) * (VD / 64);
-  const bool none = l == 0;
-  for (int d = 0; d < VD / 64; ++d) o[d] = static_cast<T>(none ? 0.0f : acc[d] / l);
-  if (p.lse && (threadIdx.x & 63) == 0)
-    p.lse[static_cast<uint64_t>(row) * p.n_heads + head] = none ? -__builtin_inff() : (m + __log2f(l)) * kLn2;
+  if (p.n_requests > 1) {
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint64_t u = shfl_up64(total, d);
+      if (static_cast<int>(lane) >= d) total += u;
+    }
+    total = shfl64(total, 63);
+  } else {
+    total = shfl64(total, 0);
+  }
+  const uint64_t part = (total * p.units + p.target - 1) / p.target;
+  if (part >= 0x7fffff00u) return 0x7fffffffu;
+  const uint32_t k = static_cast<uint32_t>(part);
+  return ((k > kMinPart ? k : kMinPart) + 63) & ~63u;
+}
+
+// Item `b` of the batch (every wave finds it for itself); kBase: b counts tiles
+// x units, and the item is its first part.
+template <bool kBase>
+__device__ __forceinline__ bool find_work(const AttnParams& p, uint32_t b, Work* out) {
+  const uint32_t lane = threadIdx.x & 63, part = part_keys(p);
+  uint32_t items_before = 0, slots_before = 0;
+  for (uint32_t r0 = 0; r0 < p.n_requests; r0 += 64) {
+    const RequestWork w = request_work(p, r0 + lane);
+    const uint32_t s = splits_of(w.range, part), base = w.tiles * p.units;
+    const uint32_t items = kBase ? base : base * s, slots = s > 1 ? base * s : 0;
+    uint32_t ends = items, slot_ends = slots;
+    if (p.n_requests > 1)
+      for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t u = __shfl_up(ends, d), v = __shfl_up(slot_ends, d);
+        if (static_cast<int>(lane) >= d) {
+          ends += u;
+          slot_ends += v;
+        }
+      }
+    ends += items_before;
+    slot_ends += slots_before;
+    const uint64_t past = __ballot(ends > b);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      const uint32_t local = b - (__shfl(ends, l) - __shfl(items, l));
+      out->r = r0 + l;
+      out->n_splits = __shfl(s, l);
+      const uint32_t tiles = __shfl(w.tiles, l);
+      const uint32_t rest = kBase ? local : local / out->n_splits;
+      out->split = kBase ? 0 : local - rest * out->n_splits;
+      const uint32_t t = rest / p.units;
+      out->unit = rest - t * p.units;
+      out->tile = tiles - 1 - t;  // the last tokens see the most keys: first
+      out->slot = __shfl(slot_ends, l) - __shfl(slots, l) + rest * out->n_splits;
+      return true;
+    }
+    items_before = __shfl(ends, 63);
+    slots_before = __shfl(slot_ends, 63);
+  }
+  return false;
+}
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// C[32 x 32] += A[32 x 16] B[16 x 32].  Lane l = 32 h + c holds row c of A and
+// column c of B at k = 8 h .. 8 h + 7, and column c of C at rows
+// 8 (e / 4) + 4 h + e % 4 for e = 0..15.
+template <typename T>
+__device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c);
+template <>
+__device__ __forceinline__ f32x16 mfma<__bf16>(s16x8 a, s16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ f32x16 mfma<_Float16>(s16x8 a, s16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
 template <typename T>
-hipError_t launch_rows(const AttnParams& p, hipStream_t s) {
-  const dim3 grid(p.n_tokens, (p.n_heads + kRowThreads / 64 - 1) / (kRowThreads / 64));
-  if (p.k_dim == 64) hipLaunchKernelGGL((k_attend_rows<T, 64, 64>), grid, dim3(kRowThreads), 0, s, p);
-  else if (p.k_dim == 128) hipLaunchKernelGGL((k_attend_rows<T, 128, 128>), grid, dim3(kRowThreads), 0, s, p);
-  else hipLaunchKernelGGL((k_attend_rows<T, 576, 512>), grid, dim3(kRowThreads), 0, s, p);
+__device__ __forceinline__ s16x8 to_half(const float* x) {
+  typedef T T8 __attribute__((ext_vector_type(8)));
+  T8 y;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = static_cast<T>(x[i]);
+  return __builtin_bit_cast(s16x8, y);
+}
+
+#define BSR_LDS __attribute__((address_space(3)))
+__device__ __forceinline__ uint32_t lds_at(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((BSR_LDS const uint8_t*)p));
+}
+
+// 64 lanes x 16 bytes from memory to LDS, lane after lane from `lds` on
+// (wave-uniform), past the registers.  The compiler does not see it: it is waited for by
+// loads_done, and every reader lies behind that and a barrier.
+__device__ __forceinline__ void load_to_lds(const uint8_t* src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory");
+}
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+__device__ __forceinline__ s16x8 lds_row16(uint32_t at) {
+  return *(const BSR_LDS s16x8*)(uintptr_t)at;
+}
+// Transposed read: every 16 lanes read a block of four rows (keys) of 16
+// 16-bit values, lane i the four at row i / 4, column 4 (i % 4); lane i gets column i.
+__device__ __forceinline__ s16x4 lds_columns(uint32_t at) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((BSR_LDS s16x4*)(uintptr_t)at);
+}
+
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// The bits of a row's tree mask from key offset `off` of the request's rows on,
+// ones before them.
+__device__ __forceinline__ uint64_t tree_bits(const AttnParams& p, const uint64_t* mask, int off) {
+  if (off <= -64) return ~0ull;
+  if (off < 0) return (mask[0] << -off) | ((1ull << -off) - 1);
+  const uint32_t w = off >> 6, sh = off & 63;
+  if (w >= p.tree_words) return 0;
+  uint64_t bits = mask[w] >> sh;
+  if (sh && w + 1 < p.tree_words) bits |= mask[w + 1] << (64 - sh);
+  return bits;
+}
+
+// Bits [lo, hi) of 64, both taken into 0..64.
+__device__ __forceinline__ uint64_t bit_range(int lo, int hi) {
+  lo = min(max(lo, 0), 64);
+  hi = min(max(hi, 0), 64);
+  if (lo >= hi) return 0;
+  const uint64_t to = hi == 64 ? ~0ull : (1ull << hi) - 1;
+  return to & (~0ull << lo);
+}
+
+// A wave's 32 query rows, one per lane of either half.
+struct TileRows {
+  bool real;         // the row exists
+  int i;             // of the request
+  uint32_t head;
+  Row see;
+  float slope2;      // slope x log2(e)
+};
+
+__device__ __forceinline__ TileRows tile_row(const AttnParams& p, const Request& q, const Work& w, uint32_t row) {
+  TileRows t;
+  const uint32_t per_kv = p.n_heads / p.n_kv_heads, chunks = p.units / p.n_kv_heads;
+  const uint32_t kv = w.unit / chunks, chunk = w.unit - kv * chunks;
+  const uint32_t tok = row / p.tile_heads, hd = chunk * kTileRows + row - tok * p.tile_heads;
+  t.i = static_cast<int>(w.tile * p.tile_tokens + tok);
+  t.real = tok < p.tile_tokens && hd < per_kv && t.i < q.rows;
+  t.head = kv * per_kv + hd;
+  t.see = Row{0x7fffffff, 0, 0, nullptr};
+  t.slope2 = 0;
+  if (t.real) {
+    t.see = row_of(p, q, w.r, t.i);
+    t.see.lo = max(t.see.lo, 0);
+    t.see.hi = min(t.see.hi, q.n);
+    if (p.slopes) t.slope2 = p.slopes[t.head] * kLog2e;
+  }
+  return t;
+}
+
+__device__ __forceinline__ int wave_min(int x) {
+  for (int d = 32; d; d >>= 1) x = min(x, __shfl_xor(x, d));
+  return x;
+}
+__device__ __forceinline__ int wave_max(int x) {
+  for (int d = 32; d; d >>= 1) x = max(x, __shfl_xor(x, d));
+  return x;
+}
+
+// Scores (times log2(e)) of a lane's keys j0 + 8 (e / 4) + e % 4, j0 = the
+// first key of the 32 plus 4 h, from their products.  Without cap and bias the products stay as they
+// are, and `unit` (scale x log2(e)) goes into the exponent.
+struct ScoreMods {
+  float unit;       // scale x log2(e)
+  float cap2;       // softcap x log2(e), 0 without
+  float in_cap;     // 2 log2(e) scale / softcap: tanh(x) = 1 - 2 / (2^(2 x log2 e) + 1)
+};
+
+__device__ __forceinline__ ScoreMods score_mods(const AttnParams& p) {
+  ScoreMods m;
+  m.unit = p.scale * kLog2e;
+  m.cap2 = p.softcap * kLog2e;
+  m.in_cap = p.softcap > 0 ? 2 * kLog2e * p.scale / p.softcap : 0;
+  return m;
+}
+
+__device__ __forceinline__ void modify(const ScoreMods& m, float slope2, int pos, int j0, f32x16& s) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    float x = s[e];
+    if (m.cap2 > 0) x = m.cap2 - 2 * m.cap2 * __builtin_amdgcn_rcpf(exp2_(x * m.in_cap) + 1);
+    else x *= m.unit;
+    s[e] = x - slope2 * static_cast<float>(abs(pos - (j0 + 8 * (e / 4) + e % 4)));
+  }
+}
+
+constexpr float kRise = 8;  // the running maximum follows a rise of more than this (weights up to 2^8 until then)
+
+// One tile's scores of a lane's row to weights: s holds 16 (kSubs times) scores,
+// `unit` what is left to multiply them by.  Returns whether any row of the
+// wave rescales, and the lane's factor in *back.
+template <int kSubs>
+__device__ __forceinline__ bool weigh(f32x16 (&s)[kSubs], float unit, float& m, float& l, float* back) {
+  float top = -__builtin_inff();
+#pragma unroll
+  for (int u = 0; u < kSubs; ++u)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
+  top = fmaxf(top, other_half(top)) * unit;
+  const bool rise = __any(top > m + kRise);
+  *back = 1;
+  if (rise) {
+    const float m1 = fmaxf(m, top);
+    *back = m > -__builtin_inff() ? exp2_(m - m1) : 0.0f;
+    l *= *back;
+    m = m1;
+  }
+  const float from = m > -__builtin_inff() ? m : 0.0f;
+  float sum = 0;
+#pragma unroll
+  for (int u = 0; u < kSubs; ++u)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[u][e] = exp2_(__builtin_fmaf(s[u][e], unit, -from));
+      sum += s[u][e];
+    }
+  l += sum;
+  return rise;
+}
+
+// Where a tile's row goes: the output, or a partial result.
+struct Sink {
+  bool part;
+  uint32_t slot;
+};
+
+template <typename T>
+__device__ __forceinline__ void put4(const AttnParams& p, const Request& q, const TileRows& t, const Sink& k, uint32_t row,
+                                     uint32_t d, f32x4 x) {
+  if (k.part) {
+    *reinterpret_cast<f32x4*>(p.part + (static_cast<uint64_t>(k.slot) * kTileRows + row) * p.v_dim + d) = x;
+  } else {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    T4 y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = static_cast<T>(x[i]);
+    *reinterpret_cast<T4*>(p.out + (q.first + t.i) * p.out_token + t.head * p.out_head + d * sizeof(T)) = y;
+  }
+}
+
+__device__ __forceinline__ void put_stats(const AttnParams& p, const Request& q, const TileRows& t, const Sink& k,
+                                          uint32_t row, float m, float l) {
+  if (k.part) {
+    float* at = p.part_ml + (static_cast<uint64_t>(k.slot) * kTileRows + row) * 2;
+    at[0] = m;
+    at[1] = l;
+  } else if (p.lse) {
+    p.lse[static_cast<uint64_t>(q.first + t.i) * p.n_heads + t.head] = l == 0 ? -__builtin_inff() : (m + __log2f(l)) * kLn2;
+  }
+}
+
+// Rows whose result is not finite saw an infinity or a NaN, or it lay where they see
+// nothing and met a weight of zero: these are done again over the keys [lo, hi), reading what
+// they see alone.
+template <typename T, int KD, int VD>
+__device__ void redo_row(const AttnParams& p, const Request& q, const Work& w, const Sink& k, uint32_t row, int lo, int hi) {
+  constexpr int kPer = VD / 64;
+  const TileRows t = tile_row(p, q, w, row);
+  if (!t.real) return;
+  float m, l, acc[kPer];
+  attend_row<T, KD, VD>(p, q, t.see, t.i, t.head, max(lo, t.see.lo), min(hi, t.see.hi), m, l, acc);
+  const uint32_t d0 = (threadIdx.x & 63) * kPer;
+  for (int d = 0; d < kPer; ++d) {
+    if (k.part) p.part[(static_cast<uint64_t>(k.slot) * kTileRows + row) * VD + d0 + d] = acc[d];
+    else
+      reinterpret_cast<T*>(p.out + (q.first + t.i) * p.out_token + t.head * p.out_head)[d0 + d] =
+          static_cast<T>(l == 0 ? 0.0f : acc[d] / l);
+  }
+  if ((threadIdx.x & 63) == 0) put_stats(p, q, t, k, row, m, l);
+}
+
+// Part `split` of the keys [lo, hi): whole steps of 64 keys.
+__device__ __forceinline__ void cut(const Work& w, int lo, int hi, int* k0, int* k1) {
+  if (hi < lo) hi = lo;
+  const uint32_t len = hi - lo;
+  const uint32_t per = ((len + w.n_splits - 1) / w.n_splits + 63) & ~63u;
+  const uint64_t at = static_cast<uint64_t>(per) * w.split;
+  *k0 = at < len ? lo + static_cast<int>(at) : hi;
+  *k1 = at + per < len ? lo + static_cast<int>(at + per) : hi;
+}
+
+// The record offset of a key, and whether its block lies in the pool; keys past the
+// part's last are read as that one (the rows do not see them).
+struct KeyLoad {
+  int j;
+  uint32_t block;
+  int32_t id;
+};
+__device__ __forceinline__ KeyLoad key_load(const AttnParams& p, const Request& q, int j, int last) {
+  KeyLoad k;
+  k.j = min(j, last);
+  k.block = p.div_block.div(k.j);
+  k.id = q.table[k.block];
+  return k;
+}
+__device__ __forceinline__ bool key_offset(const AttnParams& p, const KeyLoad& k, int64_t* off) {
+  const bool ok = k.id >= 0 && static_cast<uint32_t>(k.id) < p.pool_blocks;
+  *off = ok ? static_cast<int64_t>(k.id) * p.block_bytes + static_cast<int64_t>(k.j - k.block * p.div_block.d) * p.record_bytes : 0;
+  return ok;
+}
+
+// ---------------------------------------------------------------------------
+// KV heads of 64 or 128: four waves of 32 query rows each, 64 keys a step.
+//
+// S^T = K Q^T, so a lane holds one query row's scores of 32 keys: the softmax
+// stays in the lane but for one exchange with the other half.  The
+// weights then are the B operand of O^T = V^T P^T as they lie, since the order
+// of the keys within a product is free: lane half h takes keys 4 h .. 4 h + 3
+// and 8 + 4 h .. of every 16, and V^T, read transposed from LDS, follows.
+// O^T keeps a query row per lane too, so rescaling is a product with a lane's
+// own factor.
+//
+// K and V lie in LDS row by row, their 16-byte units permuted by the row, so
+// that neither the reads of 16 rows at one place nor the transposed reads of 8 rows
+// meet in a bank.  Two buffers: step t + 1 is loaded, past the registers, while t is computed.
+// ---------------------------------------------------------------------------
+constexpr int kAttnThreads = 256;
+
+template <int D>
+__device__ __forceinline__ uint32_t unit_swap(uint32_t row) {
+  if (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+  return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+}
+
+template <typename T, int D, bool kMods>
+__global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) {
+  constexpr int kStep = 64, kUnits = D / 8, kTileBytes = kStep * D * 2;
+  constexpr int kRowsPerLoad = 64 / kUnits, kLoads = kStep / 4 / kRowsPerLoad;  // per wave, K and V each
+  __shared__ __attribute__((aligned(1024))) uint8_t kv_tiles[2][2][kTileBytes];
+  __shared__ int64_t offsets[2][kStep];
+  __shared__ uint64_t outside[4];
+  __shared__ int ranges[2][4];
+  __shared__ uint32_t redo[4];
+
+  Work w;
+  if (!find_work<false>(p, blockIdx.x, &w)) return;
+  const Request q = request_of(p, w.r);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const uint32_t kv = w.unit / (p.units / p.n_kv_heads);
+  const uint32_t row = wave * 32 + col;
+  const TileRows t = tile_row(p, q, w, row);
+  const bool active = __any(t.real);
+  // keys that all of the wave's rows see without a look at their masks
+  const int open_lo = wave_max(t.real ? t.see.lo : 0);
+  const int open_hi = wave_min(!t.real ? 0x7fffffff : p.tree ? min(t.see.hi, q.base) : t.see.hi);
+  const int wave_lo = wave_min(t.see.lo), wave_hi = wave_max(t.see.hi);
+  if (lane == 0) {
+    ranges[0][wave] = wave_lo;
+    ranges[1][wave] = wave_hi;
+    redo[wave] = 0;
+  }
+  barrier();
+  int lo = ranges[0][0], hi = ranges[1][0], k0, k1;
+  for (int i = 1; i < 4; ++i) {
+    lo = min(lo, ranges[0][i]);
+    hi = max(hi, ranges[1][i]);
+  }
+  cut(w, lo, hi, &k0, &k1);
+  const int steps = (k1 - k0 + kStep - 1) / kStep;
+
+  s16x8 qf[D / 16];
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    qf[s] = s16x8{};
+    if (t.real)
+      qf[s] = *reinterpret_cast<const s16x8*>(p.q + (q.first + t.i) * p.q_token + t.head * p.q_head + s * 32 + half * 16);
+  }
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
+  float m = -__builtin_inff(), l = 0;
+  const ScoreMods mods = score_mods(p);
+
+  const uint8_t* k_base = p.k_pool + kv * (2 * D);
+  const uint8_t* v_base = p.v_pool + kv * (2 * D);
+  const uint32_t tiles_at = lds_at(&kv_tiles[0][0][0]);
+  // loading: the wave's rows of a step, kRowsPerLoad at a time
+  const uint32_t load_row = wave * (kStep / 4) + lane / kUnits;
+  auto load_step = [&](int buf, int slot) {
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const uint32_t r = load_row + n * kRowsPerLoad;
+      const int64_t off = offsets[slot][r] + (((lane % kUnits) ^ unit_swap<D>(r)) * 16);
+      const uint32_t to = tiles_at + buf * (2 * kTileBytes) + (wave * (kStep / 4) + n * kRowsPerLoad) * (D * 2);
+      load_to_lds(k_base + off, to);
+      load_to_lds(v_base + off, to + kTileBytes);
+    }
+  };
+  KeyLoad next{};
+  auto put_offsets = [&](int step) {  // by wave 0
+    int64_t off;
+    const bool ok = key_offset(p, next, &off);
+    offsets[step & 1][lane] = off;
+    const uint64_t bad = ~__ballot(ok);
+    if (lane == 0) outside[step & 3] = bad;
+  };
+
+  if (steps > 0) {
+    if (wave == 0) {
+      next = key_load(p, q, k0 + lane, k1 - 1);
+      put_offsets(0);
+      if (steps > 1) next = key_load(p, q, k0 + kStep + lane, k1 - 1);
+    }
+    barrier();
+    if (wave == 0 && steps > 1) put_offsets(1);
+    load_step(0, 0);
+    if (wave == 0 && steps > 2) next = key_load(p, q, k0 + 2 * kStep + lane, k1 - 1);
+  }
+
+  // read positions: K, row col of 32; V transposed, row 4 h + (lane % 16) / 4
+  const uint32_t k_at = col * (D * 2), k_swap = unit_swap<D>(col);
+  const uint32_t v_row = 4 * half + ((lane & 15) >> 2);
+  const uint32_t v_unit = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  uint32_t v_at[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    v_at[e] = (v_row + 8 * e) * (D * 2) + ((v_unit ^ unit_swap<D>(v_row + 8 * e)) * 16) + (lane & 1) * 8;
+
+  for (int step = 0; step < steps; ++step) {
+    loads_done();
+    barrier();
+    const int buf = step & 1;
+    if (wave == 0 && step + 2 < steps) put_offsets(step + 2);
+    if (step + 1 < steps) load_step(buf ^ 1, buf ^ 1);
+    if (wave == 0 && step + 3 < steps) next = key_load(p, q, k0 + (step + 3) * kStep + lane, k1 - 1);
+    if (!active) continue;
+    const int j0 = k0 + step * kStep;
+    if (j0 + kStep <= wave_lo || j0 >= wave_hi) continue;
+    const uint32_t k_tile = tiles_at + buf * (2 * kTileBytes), v_tile = k_tile + kTileBytes;
+
+    f32x16 s[2] = {};
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n)
+        s[u] = mfma<T>(lds_row16(k_tile + u * 32 * (D * 2) + k_at + (((2 * n + half) ^ k_swap) * 16)), qf[n], s[u]);
+    float unit = mods.unit;
+    if (kMods) {
+      unit = 1;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) modify(mods, t.slope2, t.see.pos, j0 + 32 * u + 4 * half, s[u]);
+    }
+    const uint64_t bad = outside[step & 3];
+    if (j0 < open_lo || j0 + kStep > open_hi || bad || j0 + kStep > k1) {
+      uint64_t see = bit_range(t.see.lo - j0, min(t.see.hi, k1) - j0) & ~bad;
+      if (p.tree && t.real) see &= tree_bits(p, t.see.mask, j0 - q.base);
+      see >>= 4 * half;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!(see >> (32 * u + 8 * (e / 4) + e % 4) & 1)) s[u][e] = -__builtin_inff();
+    }
+    float back;
+    if (weigh<2>(s, unit, m, l, &back)) {
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) o[d] *= back;
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[u][8 * n + e];
+        const s16x8 pf = to_half<T>(x);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) {
+          const uint32_t at = v_tile + (32 * u + 16 * n) * (D * 2);
+          const s16x4 a = lds_columns(at + (v_at[0] ^ (d * 64))), b = lds_columns(at + (v_at[1] ^ (d * 64)));
+          o[d] = mfma<T>(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), pf, o[d]);
+        }
+      }
+  }
+
+  const Sink sink{w.n_splits > 1, w.slot + w.split};
+  l += other_half(l);
+  const float inv = sink.part ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
+  float zero = 0;  // NaN where a result is not finite
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) {
+    o[d] *= inv;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) zero += o[d][e] * 0.0f;
+  }
+  zero += other_half(zero) + l * 0.0f;
+  const bool again = t.real && !(zero == 0);
+  const uint32_t mine = static_cast<uint32_t>(__ballot(again));
+  if (t.real && !again) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        put4<T>(p, q, t, sink, row, 32 * d + 8 * e + 4 * half, f32x4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]});
+    if (half == 0) put_stats(p, q, t, sink, row, m, l);
+  }
+  for (uint32_t left = mine; left; left &= left - 1)
+    redo_row<T, D, D>(p, q, w, sink, wave * 32 + __builtin_ctz(left), k0, k1);
+}
+
+// ---------------------------------------------------------------------------
+// Latent records of 576, the first 512 the value: one tile serves K and V.
+//
+// Four waves; 32 keys a step.  Wave w scores query rows 32 w .. 32 w + 31, its queries in
+// registers, and leaves their weights in LDS; then it sums values 128 w ..
+// 128 w + 127 of all 128 rows, so that a record is read for the products with V once.  Scores
+// of step t + 1 and values of step t share a stretch between two barriers, and
+// step t + 2 is loaded meanwhile.
+// ---------------------------------------------------------------------------
+template <typename T, bool kMods>
+__global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThreads, 1) void k_attend_latent(AttnParams p) {
+  constexpr int KD = 576, VD = 512, kStep = 32, kUnits = KD / 8, kRowBytes = KD * 2, kTileBytes = kStep * kRowBytes;
+  constexpr int kBufs = 3, kLoads = kStep * kUnits / kAttnThreads;  // 9 per wave
+  __shared__ __attribute__((aligned(1024))) uint8_t tiles[kBufs][kTileBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t weights[2][4][2][1024];  // [step][rows / 32][16 keys][lane]
+  __shared__ float backs[2][kTileRows];
+  __shared__ uint32_t rises[2][4];
+  __shared__ float stats[2][kTileRows];
+  __shared__ int64_t offsets[2][kStep];
+  __shared__ uint32_t outside[4];
+  __shared__ int ranges[2][4];
+  __shared__ uint32_t redo[4];
+
+  Work w;
+  if (!find_work<false>(p, blockIdx.x, &w)) return;
+  const Request q = request_of(p, w.r);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const uint32_t row = wave * 32 + col;
+  const TileRows t = tile_row(p, q, w, row);
+  const bool active = __any(t.real);
+  const int open_lo = wave_max(t.real ? t.see.lo : 0);
+  const int open_hi = wave_min(!t.real ? 0x7fffffff : p.tree ? min(t.see.hi, q.base) : t.see.hi);
+  const int wave_lo = wave_min(t.see.lo), wave_hi = wave_max(t.see.hi);
+  if (lane == 0) {
+    ranges[0][wave] = wave_lo;
+    ranges[1][wave] = wave_hi;
+    redo[wave] = 0;
+  }
+  barrier();
+  int lo = ranges[0][0], hi = ranges[1][0], k0, k1;
+  for (int i = 1; i < 4; ++i) {
+    lo = min(lo, ranges[0][i]);
+    hi = max(hi, ranges[1][i]);
+  }
+  cut(w, lo, hi, &k0, &k1);
+  const int steps = (k1 - k0 + kStep - 1) / kStep;
+  // row blocks with any row: a tile's rows are its first
+  const uint32_t rows = min(p.tile_tokens, q.rows - w.tile * p.tile_tokens) * p.tile_heads;
+  const int blocks = __builtin_amdgcn_readfirstlane((rows + 31) / 32);
+
+  s16x8 qf[KD / 16];
+#pragma unroll
+  for (int s = 0; s < KD / 16; ++s) {
+    qf[s] = s16x8{};
+    if (t.real)
+      qf[s] = *reinterpret_cast<const s16x8*>(p.q + (q.first + t.i) * p.q_token + t.head * p.q_head + s * 32 + half * 16);
+  }
+  f32x16 o[4][4];
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int d = 0; d < 4; ++d) o[b][d] = f32x16{};
+  float m = -__builtin_inff(), l = 0;
+  const ScoreMods mods = score_mods(p);
+
+  const uint32_t tiles_at = lds_at(&tiles[0][0]), weights_at = lds_at(&weights[0][0][0][0]);
+  auto load_step = [&](int buf, int slot) {
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const uint32_t u = (wave * kLoads + n) * 64 + lane, r = u / kUnits, c = u - r * kUnits;
+      const uint32_t from = (c & ~7u) | ((c ^ unit_swap<64>(r)) & 7);
+      load_to_lds(p.k_pool + offsets[slot][r] + from * 16, tiles_at + buf * kTileBytes + (wave * kLoads + n) * 1024);
+    }
+  };
+  KeyLoad next{};
+  auto put_offsets = [&](int step) {  // by wave 0, lanes 0..31
+    int64_t off;
+    const bool ok = key_offset(p, next, &off);
+    if (lane < kStep) offsets[step & 1][lane] = off;
+    const uint32_t bad = ~static_cast<uint32_t>(__ballot(ok));
+    if (lane == 0) outside[step & 3] = bad;
+  };
+
+  const uint32_t k_at = col * kRowBytes, k_swap = unit_swap<64>(col);
+  const uint32_t v_row = 4 * half + ((lane & 15) >> 2);
+  const uint32_t v_unit = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  uint32_t v_at[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    v_at[e] = (v_row + 8 * e) * kRowBytes + wave * 256 + ((v_unit ^ unit_swap<64>(v_row + 8 * e)) * 16) + (lane & 1) * 8;
+
+  auto score_step = [&](int step, int buf) {
+    const int j0 = k0 + step * kStep;
+    if (!active) return;
+    f32x16 s[1] = {}, s1 = {};
+    const uint32_t at = tiles_at + buf * kTileBytes + k_at;
+#pragma unroll
+    for (int n = 0; n < KD / 16; n += 2) {
+      const uint32_t c = 2 * n + half;
+      s[0] = mfma<T>(lds_row16(at + ((c & ~7u) * 16) + (((c ^ k_swap) & 7) * 16)), qf[n], s[0]);
+      const uint32_t c1 = c + 2;
+      s1 = mfma<T>(lds_row16(at + ((c1 & ~7u) * 16) + (((c1 ^ k_swap) & 7) * 16)), qf[n + 1], s1);
+    }
+    s[0] += s1;
+    float unit = mods.unit;
+    if (kMods) {
+      unit = 1;
+      modify(mods, t.slope2, t.see.pos, j0 + 4 * half, s[0]);
+    }
+    const uint32_t bad = outside[step & 3];
+    if (j0 < open_lo || j0 + kStep > open_hi || bad || j0 + kStep > k1) {
+      uint64_t see = bit_range(t.see.lo - j0, min(t.see.hi, k1) - j0) & ~static_cast<uint64_t>(bad);
+      if (p.tree && t.real) see &= tree_bits(p, t.see.mask, j0 - q.base);
+      see >>= 4 * half;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (!(see >> (8 * (e / 4) + e % 4) & 1)) s[0][e] = -__builtin_inff();
+    }
+    float back;
+    const bool rise = weigh<1>(s, unit, m, l, &back);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = s[0][8 * n + e];
+      *(BSR_LDS s16x8*)(uintptr_t)(weights_at + (((step & 1) * 4 + wave) * 2 + n) * 1024 + lane * 16) = to_half<T>(x);
+    }
+    if (half == 0) backs[step & 1][row] = back;
+    if (lane == 0) rises[step & 1][wave] = rise;
+  };
+  auto value_step = [&](int step, int buf) {
+    s16x8 v[2][4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const uint32_t at = tiles_at + buf * kTileBytes + 16 * n * kRowBytes;
+        const s16x4 a = lds_columns(at + (v_at[0] ^ ((d & 1) * 64)) + (d >> 1) * 128);
+        const s16x4 b = lds_columns(at + (v_at[1] ^ ((d & 1) * 64)) + (d >> 1) * 128);
+        v[n][d] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      if (b >= blocks) break;
+      if (rises[step & 1][b]) {
+        const float back = backs[step & 1][b * 32 + col];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[b][d] *= back;
+      }
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const s16x8 pf = lds_row16(weights_at + (((step & 1) * 4 + b) * 2 + n) * 1024 + lane * 16);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[b][d] = mfma<T>(v[n][d], pf, o[b][d]);
+      }
+    }
+  };
+
+  if (steps > 0) {
+    if (wave == 0) {
+      next = key_load(p, q, k0 + lane, k1 - 1);
+      put_offsets(0);
+      if (steps > 1) {
+        next = key_load(p, q, k0 + kStep + lane, k1 - 1);
+        put_offsets(1);
+      }
+      if (steps > 2) next = key_load(p, q, k0 + 2 * kStep + lane, k1 - 1);
+    }
+    barrier();
+    load_step(0, 0);
+    if (steps > 1) load_step(1, 1);
+    loads_done();
+    barrier();
+    if (wave == 0 && steps > 2) {
+      put_offsets(2);
+      if (steps > 3) next = key_load(p, q, k0 + 3 * kStep + lane, k1 - 1);
+    }
+    score_step(0, 0);
+  }
+  int buf = 0;
+  for (int step = 0; step < steps; ++step) {
+    loads_done();
+    barrier();  // step + 1 lies in LDS, the weights of this step too; the buffer of step - 1 is free
+    const int buf1 = buf == 2 ? 0 : buf + 1, buf2 = buf1 == 2 ? 0 : buf1 + 1;
+    if (wave == 0 && step + 3 < steps) put_offsets(step + 3);
+    if (step + 2 < steps) load_step(buf2, step & 1);
+    if (wave == 0 && step + 4 < steps) next = key_load(p, q, k0 + (step + 4) * kStep + lane, k1 - 1);
+    if (step + 1 < steps) score_step(step + 1, buf1);
+    value_step(step, buf);
+    buf = buf1;
+  }
+
+  const Sink sink{w.n_splits > 1, w.slot + w.split};
+  l += other_half(l);
+  if (half == 0) {
+    stats[0][row] = m;
+    stats[1][row] = l;
+  }
+  barrier();
+  uint32_t bad_rows = 0;  // of the wave's values, by row block, found before any of them is stored
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    if (b >= blocks) break;
+    const float lb = stats[1][b * 32 + col];
+    const float inv = sink.part ? 1.0f : lb == 0 ? 0.0f : 1.0f / lb;
+    float zero = lb * 0.0f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      o[b][d] *= inv;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) zero += o[b][d][e] * 0.0f;
+    }
+    zero += other_half(zero);
+    bad_rows = static_cast<uint32_t>(__ballot(!(zero == 0)));
+    if (lane == 0 && bad_rows) atomicOr(&redo[b], bad_rows);
+  }
+  barrier();
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    if (b >= blocks) break;
+    const TileRows tb = tile_row(p, q, w, b * 32 + col);
+    if (!tb.real || (redo[b] >> col & 1)) continue;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        put4<T>(p, q, tb, sink, b * 32 + col, 128 * wave + 32 * d + 8 * e + 4 * half,
+                f32x4{o[b][d][4 * e], o[b][d][4 * e + 1], o[b][d][4 * e + 2], o[b][d][4 * e + 3]});
+    if (half == 0 && wave == 0) put_stats(p, q, tb, sink, b * 32 + col, stats[0][b * 32 + col], stats[1][b * 32 + col]);
+  }
+  for (int b = 0; b < blocks; ++b)
+    for (uint32_t left = redo[b]; left; left &= left - 1) {
+      const uint32_t c = __builtin_ctz(left);
+      if ((c & 3) == static_cast<uint32_t>(wave)) redo_row<T, KD, VD>(p, q, w, sink, b * 32 + c, k0, k1);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Joins the parts of a row: sums and maxima as the running softmax would have
+// joined them, always in the order of the parts.
+// ---------------------------------------------------------------------------
+constexpr int kJoinThreads = 128;
+
+template <typename T, int VD>
+__global__ __launch_bounds__(kJoinThreads) void k_attend_join(AttnParams p, uint32_t rows_per) {
+  constexpr int kVecs = VD / 4, kSide = kJoinThreads / kVecs;  // threads of a row; rows side by side
+  Work w;
+  if (!find_work<true>(p, blockIdx.x, &w) || w.n_splits < 2) return;
+  const Request q = request_of(p, w.r);
+  const uint32_t d = threadIdx.x % kVecs * 4;
+  for (uint32_t row = blockIdx.y * rows_per + threadIdx.x / kVecs; row < (blockIdx.y + 1) * rows_per; row += kSide) {
+    const TileRows t = tile_row(p, q, w, row);
+    if (!t.real) continue;
+    const float* ml = p.part_ml + (static_cast<uint64_t>(w.slot) * kTileRows + row) * 2;
+    const float* part = p.part + (static_cast<uint64_t>(w.slot) * kTileRows + row) * VD + d;
+    float m = -__builtin_inff();
+    for (uint32_t s = 0; s < w.n_splits; ++s) m = fmaxf(m, ml[s * kTileRows * 2]);
+    const float from = m > -__builtin_inff() ? m : 0.0f;
+    float l = 0;
+    f32x4 x{};
+    for (uint32_t s = 0; s < w.n_splits; ++s) {
+      const float ls = ml[s * kTileRows * 2 + 1];
+      if (ls == 0) continue;
+      const float f = exp2_(ml[s * kTileRows * 2] - from);
+      l += f * ls;
+      x += f * *reinterpret_cast<const f32x4*>(part + static_cast<uint64_t>(s) * kTileRows * VD);
+    }
+    const Sink sink{false, 0};
+    x *= l == 0 ? 0.0f : 1.0f / l;
+    put4<T>(p, q, t, sink, row, d, x);
+    if (d == 0) put_stats(p, q, t, sink, row, m, l);
+  }
+}
+
+template <typename T, int VD>
+hipError_t launch_join(const AttnParams& p, uint32_t base, hipStream_t s) {
+  const uint32_t rows = p.tile_tokens * p.tile_heads, side = kJoinThreads / (VD / 4);
+  // rows of a workgroup: one pass of its threads where tiles are few, more where their number alone fills the GPU
+  uint32_t per = side;
+  while (per < rows && static_cast<uint64_t>(base) * ((rows + per - 1) / per) > 8192) per *= 2;
+  hipLaunchKernelGGL((k_attend_join<T, VD>), dim3(base, (rows + per - 1) / per), dim3(kJoinThreads), 0, s, p, per);
   return hipGetLastError();
+}
+
+template <typename T, bool kMods>
+hipError_t launch_tiles(const AttnParams& p, hipStream_t s) {
+  const AttnTiling t = attn_tiling(p.n_requests, p.n_tokens, p.n_heads, p.n_kv_heads, p.v_dim, p.max_len);
+  const dim3 grid(static_cast<uint32_t>(t.base + p.target)), block(kAttnThreads);
+  if (p.k_dim == 64) hipLaunchKernelGGL((k_attend_heads<T, 64, kMods>), grid, block, 0, s, p);
+  else if (p.k_dim == 128) hipLaunchKernelGGL((k_attend_heads<T, 128, kMods>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((k_attend_latent<T, kMods>), grid, block, 0, s, p);
+  if (hipError_t e = hipGetLastError()) return e;
+  if (!p.target) return hipSuccess;
+  const uint32_t base = static_cast<uint32_t>(t.base);
+  return p.v_dim == 64 ? launch_join<T, 64>(p, base, s) : p.v_dim == 128 ? launch_join<T, 128>(p, base, s) : launch_join<T, 512>(p, base, s);
 }
 
 }  // namespace
 
+AttnTiling attn_tiling(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads, uint32_t n_kv_heads, uint32_t v_dim,
+                       uint32_t max_len) {
+  AttnTiling t{};
+  const uint32_t per_kv = n_heads / n_kv_heads;
+  t.tile_heads = per_kv < kTileRows ? per_kv : kTileRows;
+  t.tile_tokens = kTileRows / t.tile_heads;
+  t.units = n_kv_heads * ((per_kv + kTileRows - 1) / kTileRows);
+  // every request may end a tile early; none has a tile without a token
+  const uint64_t tiles = (n_tokens / t.tile_tokens) + static_cast<uint64_t>(n_requests < n_tokens ? n_requests : n_tokens);
+  t.base = tiles * t.units;
+  if (max_len > kMinPart) {
+    t.target = v_dim == 512 ? 256 : 512;  // workgroups that the GPU holds at once
+    const uint64_t most = t.base * ((max_len + kMinPart - 1) / kMinPart);
+    t.slots = most < 2ull * t.target ? most : 2ull * t.target;
+    t.workspace = t.slots * kTileRows * (v_dim + 2) * sizeof(float);
+  }
+  return t;
+}
+
 hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
-  return p.f16 ? launch_rows<_Float16>(p, s) : launch_rows<__bf16>(p, s);
+  const bool mods = p.softcap > 0 || p.slopes;
+  if (p.f16) return mods ? launch_tiles<_Float16, true>(p, s) : launch_tiles<_Float16, false>(p, s);
+  return mods ? launch_tiles<__bf16, true>(p, s) : launch_tiles<__bf16, false>(p, s);
 }
 
 }  // namespace bsr

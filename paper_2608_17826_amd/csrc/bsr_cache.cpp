@@ -139,8 +139,23 @@ int check_attn(const bsr_ctx* c, const bsr_attn_args* a, bsr::AttnParams* p) {
   return BSR_OK;
 }
 
+bsr::AttnTiling tiling_of(const bsr_attn_args* a) {
+  return bsr::attn_tiling(a->n_requests, a->n_tokens, a->n_heads, a->n_kv_heads, a->v_dim, a->max_len);
+}
+
 int attend(const bsr_ctx* c, const bsr_attn_args* a, bsr::AttnParams* p, void* stream) {
   if (a->n_requests == 0 || a->n_tokens == 0) return check_device(c);
+  const bsr::AttnTiling t = tiling_of(a);
+  if (t.workspace && (!a->workspace || !aligned(a->workspace, 16) || a->workspace_bytes < t.workspace))
+    return refuse(BSR_E_ARG, "workspace is NULL, not 16-byte aligned or smaller than %llu bytes",
+                  static_cast<unsigned long long>(t.workspace));
+  if (t.base + t.target >= (1ull << 24)) return refuse(BSR_E_ARG, "too many rows and heads for one launch");
+  p->tile_heads = t.tile_heads;
+  p->tile_tokens = t.tile_tokens;
+  p->units = t.units;
+  p->target = t.target;
+  p->part = static_cast<float*>(a->workspace);
+  p->part_ml = p->part + t.slots * bsr::kTileRows * a->v_dim;
   return enqueue(c, "attention", [&] { return bsr::launch_attention(*p, static_cast<hipStream_t>(stream)); });
 }
 
@@ -240,7 +255,7 @@ int bsr_cache_append(bsr_ctx* c, const bsr_append_args* a, void* stream) {
 
 uint64_t bsr_attn_workspace_bytes(bsr_ctx* c, const bsr_attn_args* a) {
   if (check_ctx(c, a) || check_attn(c, a, nullptr)) return BSR_ATTN_REFUSED;
-  return 0;
+  return tiling_of(a).workspace;
 }
 
 int bsr_attend_tree(bsr_ctx* c, const bsr_attn_args* a, void* stream) {
