@@ -138,7 +138,7 @@ __device__ void attend_row(const AttnParams& p, const Request& q, const Row& w, 
 
 
 // ---------------------------------------------------------------------------
-// The work: a tile is kTileRows query rows, tile_tokens tokens times
+// The work: a tile is up to tile_rows query rows, tile_tokens tokens times
 // tile_heads heads of one KV head, so that a key read once serves them all.
 // Where a batch has few tiles its key ranges are cut into parts, and a second
 // kernel joins them.  Every workgroup finds its item from the lengths alone:
@@ -151,6 +151,13 @@ struct Work {
   uint32_t split, n_splits;
   uint32_t slot;    // first partial result of the item's parts
 };
+
+// What is the same in every lane, into a scalar register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+  return static_cast<uint64_t>(uniform(static_cast<uint32_t>(x >> 32))) << 32 | uniform(static_cast<uint32_t>(x));
+}
 
 struct RequestWork {
   uint32_t tiles, range;  // tiles of tokens, keys that one of them can see at most
@@ -200,7 +207,7 @@ __device__ __forceinline__ uint32_t part_keys(const AttnParams& p) {
   const uint64_t part = (total * p.units + p.target - 1) / p.target;
   if (part >= 0x7fffff00u) return 0x7fffffffu;
   const uint32_t k = static_cast<uint32_t>(part);
-  return ((k > kMinPart ? k : kMinPart) + 63) & ~63u;
+  return uniform(((k > kMinPart ? k : kMinPart) + 63) & ~63u);
 }
 
 // Item `b` of the batch (every wave finds it for itself); kBase: b counts tiles
@@ -227,16 +234,16 @@ __device__ __forceinline__ bool find_work(const AttnParams& p, uint32_t b, Work*
     const uint64_t past = __ballot(ends > b);
     if (past) {
       const int l = __builtin_ctzll(past);
-      const uint32_t local = b - (__shfl(ends, l) - __shfl(items, l));
+      const uint32_t local = uniform(b - (__shfl(ends, l) - __shfl(items, l)));
       out->r = r0 + l;
-      out->n_splits = __shfl(s, l);
-      const uint32_t tiles = __shfl(w.tiles, l);
+      out->n_splits = uniform(__shfl(s, l));
+      const uint32_t tiles = uniform(__shfl(w.tiles, l));
       const uint32_t rest = kBase ? local : local / out->n_splits;
       out->split = kBase ? 0 : local - rest * out->n_splits;
       const uint32_t t = rest / p.units;
       out->unit = rest - t * p.units;
       out->tile = tiles - 1 - t;  // the last tokens see the most keys: first
-      out->slot = __shfl(slot_ends, l) - __shfl(slots, l) + rest * out->n_splits;
+      out->slot = uniform(__shfl(slot_ends, l) - __shfl(slots, l)) + rest * out->n_splits;
       return true;
     }
     items_before = __shfl(ends, 63);
@@ -267,6 +274,24 @@ __device__ __forceinline__ f32x16 mfma<_Float16>(s16x8 a, s16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// The same with the results in vector registers whatever the rest of the
+// kernel uses: the compiler keeps all of a kernel's results in accumulator registers
+// once it needs any of them, and the latent attention has none left.  The compiler
+// sees no matrix instruction here, so a value that it computed must not be an operand of the next
+// one or two, and the last product's result is read after mfma_done (a product of 8
+// passes needs 11 wait states; the waits are 20).
+template <typename T>
+__device__ __forceinline__ void mfma_first(f32x16& c, s16x8 a, s16x8 b) {
+  if (__is_same(T, __bf16)) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "v"(b));
+  else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "v"(b));
+}
+template <typename T>
+__device__ __forceinline__ void mfma_next(f32x16& c, s16x8 a, s16x8 b) {
+  if (__is_same(T, __bf16)) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
+  else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void mfma_done(f32x16& c) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(c)); }
+
 template <typename T>
 __device__ __forceinline__ s16x8 to_half(const float* x) {
   typedef T T8 __attribute__((ext_vector_type(8)));
@@ -276,6 +301,22 @@ __device__ __forceinline__ s16x8 to_half(const float* x) {
   return __builtin_bit_cast(s16x8, y);
 }
 
+// c *= f with c in accumulator registers throughout, which vector instructions do not
+// take: the plain product makes the compiler move and spill all of the latent attention's sums
+// at every step, though few steps need it.  The first wait lets products that
+// write c end, the last keeps the next one off a register just written.
+__device__ __forceinline__ void scale_accumulators(f32x16& c, float f) {
+  asm volatile("s_nop 15\n\ts_nop 3" : "+a"(c));
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    float x = c[e], y;
+    asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_mul_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(y) : "v"(f));
+    c[e] = x;
+  }
+  asm volatile("s_nop 3" : "+a"(c));
+}
+
+#define BSR_INLINE __attribute__((always_inline))
 #define BSR_LDS __attribute__((address_space(3)))
 __device__ __forceinline__ uint32_t lds_at(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((BSR_LDS const uint8_t*)p));
@@ -303,7 +344,27 @@ __device__ __forceinline__ s16x4 lds_columns(uint32_t at) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((BSR_LDS s16x4*)(uintptr_t)at);
 }
 
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// A lane's value and that of the same lane of the other half, in either order.
+struct Halves {
+  float a, b;
+};
+__device__ __forceinline__ Halves halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return {__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ float max_halves(float x) {
+  const Halves h = halves(x);
+  return fmaxf(h.a, h.b);
+}
+__device__ __forceinline__ float sum_halves(float x) {
+  const Halves h = halves(x);
+  return h.a + h.b;
+}
+
+// Instructions of one kind next in the order of the block: matrix products,
+// reads of LDS, anything of the vector unit.
+constexpr int kMatrix = 0x8, kLdsRead = 0x100, kVector = 0x2;
+#define BSR_ORDER(kind, n) __builtin_amdgcn_sched_group_barrier(kind, n, 0)
 
 // The bits of a row's tree mask from key offset `off` of the request's rows on,
 // ones before them.
@@ -339,7 +400,7 @@ __device__ __forceinline__ TileRows tile_row(const AttnParams& p, const Request&
   TileRows t;
   const uint32_t per_kv = p.n_heads / p.n_kv_heads, chunks = p.units / p.n_kv_heads;
   const uint32_t kv = w.unit / chunks, chunk = w.unit - kv * chunks;
-  const uint32_t tok = row / p.tile_heads, hd = chunk * kTileRows + row - tok * p.tile_heads;
+  const uint32_t tok = row / p.tile_heads, hd = chunk * p.tile_heads + row - tok * p.tile_heads;
   t.i = static_cast<int>(w.tile * p.tile_tokens + tok);
   t.real = tok < p.tile_tokens && hd < per_kv && t.i < q.rows;
   t.head = kv * per_kv + hd;
@@ -392,36 +453,35 @@ __device__ __forceinline__ void modify(const ScoreMods& m, float slope2, int pos
 
 constexpr float kRise = 8;  // the running maximum follows a rise of more than this (weights up to 2^8 until then)
 
-// One tile's scores of a lane's row to weights: s holds 16 (kSubs times) scores,
-// `unit` what is left to multiply them by.  Returns whether any row of the
-// wave rescales, and the lane's factor in *back.
+// The running maximum m and sum l of a lane's row after 16 kSubs more scores
+// (`unit` is what is left to multiply them by).  Returns whether any row of the wave rescales
+// what it has summed, and the lane's factor in *back.
 template <int kSubs>
-__device__ __forceinline__ bool weigh(f32x16 (&s)[kSubs], float unit, float& m, float& l, float* back) {
+__device__ __forceinline__ bool raise(const f32x16 (&s)[kSubs], float unit, float& m, float& l, float* back) {
   float top = -__builtin_inff();
 #pragma unroll
   for (int u = 0; u < kSubs; ++u)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
-  top = fmaxf(top, other_half(top)) * unit;
-  const bool rise = __any(top > m + kRise);
+    for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[u][e]), s[u][e + 1]);
+  top = max_halves(top) * unit;
   *back = 1;
-  if (rise) {
-    const float m1 = fmaxf(m, top);
-    *back = m > -__builtin_inff() ? exp2_(m - m1) : 0.0f;
-    l *= *back;
-    m = m1;
+  if (!__any(top > m + kRise)) return false;
+  const float m1 = fmaxf(m, top);
+  *back = m > -__builtin_inff() ? exp2_(m - m1) : 0.0f;
+  l *= *back;
+  m = m1;
+  return true;
+}
+
+// 16 scores to weights, and their sum.
+__device__ __forceinline__ float weigh(f32x16& s, float unit, float from) {
+  float sum[2] = {};
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    s[e] = exp2_(__builtin_fmaf(s[e], unit, -from));
+    sum[e & 1] += s[e];
   }
-  const float from = m > -__builtin_inff() ? m : 0.0f;
-  float sum = 0;
-#pragma unroll
-  for (int u = 0; u < kSubs; ++u)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      s[u][e] = exp2_(__builtin_fmaf(s[u][e], unit, -from));
-      sum += s[u][e];
-    }
-  l += sum;
-  return rise;
+  return sum[0] + sum[1];
 }
 
 // Where a tile's row goes: the output, or a partial result.
@@ -434,7 +494,7 @@ template <typename T>
 __device__ __forceinline__ void put4(const AttnParams& p, const Request& q, const TileRows& t, const Sink& k, uint32_t row,
                                      uint32_t d, f32x4 x) {
   if (k.part) {
-    *reinterpret_cast<f32x4*>(p.part + (static_cast<uint64_t>(k.slot) * kTileRows + row) * p.v_dim + d) = x;
+    *reinterpret_cast<f32x4*>(p.part + (static_cast<uint64_t>(k.slot) * p.tile_rows + row) * p.v_dim + d) = x;
   } else {
     typedef T T4 __attribute__((ext_vector_type(4)));
     T4 y;
@@ -447,7 +507,7 @@ __device__ __forceinline__ void put4(const AttnParams& p, const Request& q, cons
 __device__ __forceinline__ void put_stats(const AttnParams& p, const Request& q, const TileRows& t, const Sink& k,
                                           uint32_t row, float m, float l) {
   if (k.part) {
-    float* at = p.part_ml + (static_cast<uint64_t>(k.slot) * kTileRows + row) * 2;
+    float* at = p.part_ml + (static_cast<uint64_t>(k.slot) * p.tile_rows + row) * 2;
     at[0] = m;
     at[1] = l;
   } else if (p.lse) {
@@ -467,7 +527,7 @@ __device__ void redo_row(const AttnParams& p, const Request& q, const Work& w, c
   attend_row<T, KD, VD>(p, q, t.see, t.i, t.head, max(lo, t.see.lo), min(hi, t.see.hi), m, l, acc);
   const uint32_t d0 = (threadIdx.x & 63) * kPer;
   for (int d = 0; d < kPer; ++d) {
-    if (k.part) p.part[(static_cast<uint64_t>(k.slot) * kTileRows + row) * VD + d0 + d] = acc[d];
+    if (k.part) p.part[(static_cast<uint64_t>(k.slot) * p.tile_rows + row) * VD + d0 + d] = acc[d];
     else
       reinterpret_cast<T*>(p.out + (q.first + t.i) * p.out_token + t.head * p.out_head)[d0 + d] =
           static_cast<T>(l == 0 ? 0.0f : acc[d] / l);
@@ -548,9 +608,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
   const TileRows t = tile_row(p, q, w, row);
   const bool active = __any(t.real);
   // keys that all of the wave's rows see without a look at their masks
-  const int open_lo = wave_max(t.real ? t.see.lo : 0);
-  const int open_hi = wave_min(!t.real ? 0x7fffffff : p.tree ? min(t.see.hi, q.base) : t.see.hi);
-  const int wave_lo = wave_min(t.see.lo), wave_hi = wave_max(t.see.hi);
+  const int open_lo = uniform(wave_max(t.real ? t.see.lo : 0));
+  const int open_hi = uniform(wave_min(!t.real ? 0x7fffffff : p.tree ? min(t.see.hi, q.base) : t.see.hi));
+  const int wave_lo = uniform(wave_min(t.see.lo)), wave_hi = uniform(wave_max(t.see.hi));
   if (lane == 0) {
     ranges[0][wave] = wave_lo;
     ranges[1][wave] = wave_hi;
@@ -562,7 +622,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
     lo = min(lo, ranges[0][i]);
     hi = max(hi, ranges[1][i]);
   }
-  cut(w, lo, hi, &k0, &k1);
+  cut(w, uniform(lo), uniform(hi), &k0, &k1);
   const int steps = (k1 - k0 + kStep - 1) / kStep;
 
   s16x8 qf[D / 16];
@@ -583,7 +643,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
   const uint32_t tiles_at = lds_at(&kv_tiles[0][0][0]);
   // loading: the wave's rows of a step, kRowsPerLoad at a time
   const uint32_t load_row = wave * (kStep / 4) + lane / kUnits;
-  auto load_step = [&](int buf, int slot) {
+  auto load_step = [&](int buf, int slot) BSR_INLINE {
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
       const uint32_t r = load_row + n * kRowsPerLoad;
@@ -594,7 +654,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
     }
   };
   KeyLoad next{};
-  auto put_offsets = [&](int step) {  // by wave 0
+  auto put_offsets = [&](int step) BSR_INLINE {  // by wave 0
     int64_t off;
     const bool ok = key_offset(p, next, &off);
     offsets[step & 1][lane] = off;
@@ -630,24 +690,53 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
     if (wave == 0 && step + 2 < steps) put_offsets(step + 2);
     if (step + 1 < steps) load_step(buf ^ 1, buf ^ 1);
     if (wave == 0 && step + 3 < steps) next = key_load(p, q, k0 + (step + 3) * kStep + lane, k1 - 1);
-    if (!active) continue;
     const int j0 = k0 + step * kStep;
-    if (j0 + kStep <= wave_lo || j0 >= wave_hi) continue;
+    if (!active || j0 + kStep <= wave_lo || j0 >= wave_hi) continue;
     const uint32_t k_tile = tiles_at + buf * (2 * kTileBytes), v_tile = k_tile + kTileBytes;
 
+    constexpr int kN = D / 16, kD = D / 32;
+    auto k_row = [&](int u, int n) BSR_INLINE {
+      return lds_row16(k_tile + u * 32 * (D * 2) + k_at + (((2 * n + half) ^ k_swap) * 16));
+    };
+    // values of 16 keys g, dimensions 32 d ..
+    auto v_cols = [&](int g, int d) BSR_INLINE {
+      const uint32_t at = v_tile + 16 * g * (D * 2);
+      const s16x4 a = lds_columns(at + (v_at[0] ^ (d * 64))), b = lds_columns(at + (v_at[1] ^ (d * 64)));
+      return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    // reads of LDS run ahead of the products: of the second 32 keys while the
+    // first are multiplied, of the first values before the softmax
     f32x16 s[2] = {};
+    s16x8 kf[kN], vf[2][kD];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int n = 0; n < kN; ++n) kf[n] = k_row(0, n);
 #pragma unroll
-      for (int n = 0; n < D / 16; ++n)
-        s[u] = mfma<T>(lds_row16(k_tile + u * 32 * (D * 2) + k_at + (((2 * n + half) ^ k_swap) * 16)), qf[n], s[u]);
+    for (int n = 0; n < kN; ++n) {
+      s[0] = mfma<T>(kf[n], qf[n], s[0]);
+      kf[n] = k_row(1, n);
+    }
+#pragma unroll
+    for (int n = 0; n < kN; ++n) s[1] = mfma<T>(kf[n], qf[n], s[1]);
+#pragma unroll
+    for (int d = 0; d < kD; ++d) vf[0][d] = v_cols(0, d);
+    BSR_ORDER(kLdsRead, kN);
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      BSR_ORDER(kMatrix, 1);
+      BSR_ORDER(kLdsRead, 1);
+    }
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      BSR_ORDER(kMatrix, 1);
+      BSR_ORDER(kLdsRead, 1);
+    }
     float unit = mods.unit;
     if (kMods) {
       unit = 1;
 #pragma unroll
       for (int u = 0; u < 2; ++u) modify(mods, t.slope2, t.see.pos, j0 + 32 * u + 4 * half, s[u]);
     }
-    const uint64_t bad = outside[step & 3];
+    const uint64_t bad = uniform(outside[step & 3]);
     if (j0 < open_lo || j0 + kStep > open_hi || bad || j0 + kStep > k1) {
       uint64_t see = bit_range(t.see.lo - j0, min(t.see.hi, k1) - j0) & ~bad;
       if (p.tree && t.real) see &= tree_bits(p, t.see.mask, j0 - q.base);
@@ -659,29 +748,33 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
           if (!(see >> (32 * u + 8 * (e / 4) + e % 4) & 1)) s[u][e] = -__builtin_inff();
     }
     float back;
-    if (weigh<2>(s, unit, m, l, &back)) {
+    if (raise<2>(s, unit, m, l, &back)) {
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d) o[d] *= back;
+      for (int d = 0; d < kD; ++d) o[d] *= back;
     }
+    const float from = m > -__builtin_inff() ? m : 0.0f;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) {
+      l += weigh(s[u], unit, from);
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
+        const int g = 2 * u + n;
+        if (g < 3) {
+#pragma unroll
+          for (int d = 0; d < kD; ++d) vf[(g + 1) & 1][d] = v_cols(g + 1, d);
+        }
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = s[u][8 * n + e];
         const s16x8 pf = to_half<T>(x);
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) {
-          const uint32_t at = v_tile + (32 * u + 16 * n) * (D * 2);
-          const s16x4 a = lds_columns(at + (v_at[0] ^ (d * 64))), b = lds_columns(at + (v_at[1] ^ (d * 64)));
-          o[d] = mfma<T>(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), pf, o[d]);
-        }
+        for (int d = 0; d < kD; ++d) o[d] = mfma<T>(vf[g & 1][d], pf, o[d]);
       }
+    }
   }
 
   const Sink sink{w.n_splits > 1, w.slot + w.split};
-  l += other_half(l);
+  l = sum_halves(l);
   const float inv = sink.part ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
   float zero = 0;  // NaN where a result is not finite
 #pragma unroll
@@ -690,7 +783,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
 #pragma unroll
     for (int e = 0; e < 16; ++e) zero += o[d][e] * 0.0f;
   }
-  zero += other_half(zero) + l * 0.0f;
+  zero = sum_halves(zero) + l * 0.0f;
   const bool again = t.real && !(zero == 0);
   const uint32_t mine = static_cast<uint32_t>(__ballot(again));
   if (t.real && !again) {
@@ -714,15 +807,16 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
 // of step t + 1 and values of step t share a stretch between two barriers, and
 // step t + 2 is loaded meanwhile.
 // ---------------------------------------------------------------------------
-template <typename T, bool kMods>
+template <typename T, bool kMods, int kBlocks>
 __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThreads, 1) void k_attend_latent(AttnParams p) {
   constexpr int KD = 576, VD = 512, kStep = 32, kUnits = KD / 8, kRowBytes = KD * 2, kTileBytes = kStep * kRowBytes;
   constexpr int kBufs = 3, kLoads = kStep * kUnits / kAttnThreads;  // 9 per wave
+  constexpr int kN = KD / 16, kAhead = 6;
   __shared__ __attribute__((aligned(1024))) uint8_t tiles[kBufs][kTileBytes];
-  __shared__ __attribute__((aligned(16))) uint8_t weights[2][4][2][1024];  // [step][rows / 32][16 keys][lane]
-  __shared__ float backs[2][kTileRows];
+  __shared__ __attribute__((aligned(16))) uint8_t weights[2][kBlocks][2][1024];  // [step][rows / 32][16 keys][lane]
+  __shared__ float backs[2][32 * kBlocks];
   __shared__ uint32_t rises[2][4];
-  __shared__ float stats[2][kTileRows];
+  __shared__ float stats[2][32 * kBlocks];
   __shared__ int64_t offsets[2][kStep];
   __shared__ uint32_t outside[4];
   __shared__ int ranges[2][4];
@@ -733,15 +827,16 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   const Request q = request_of(p, w.r);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
+  const bool scores = wave < kBlocks;  // waves with query rows of their own
   const uint32_t row = wave * 32 + col;
   const TileRows t = tile_row(p, q, w, row);
-  const bool active = __any(t.real);
-  const int open_lo = wave_max(t.real ? t.see.lo : 0);
-  const int open_hi = wave_min(!t.real ? 0x7fffffff : p.tree ? min(t.see.hi, q.base) : t.see.hi);
-  const int wave_lo = wave_min(t.see.lo), wave_hi = wave_max(t.see.hi);
+  const int open_lo = uniform(wave_max(t.real ? t.see.lo : 0));
+  const int open_hi = uniform(wave_min(!t.real ? 0x7fffffff : p.tree ? min(t.see.hi, q.base) : t.see.hi));
+  const int wave_lo = uniform(wave_min(t.see.lo)), wave_hi = uniform(wave_max(t.see.hi));
   if (lane == 0) {
     ranges[0][wave] = wave_lo;
     ranges[1][wave] = wave_hi;
+    rises[0][wave] = rises[1][wave] = 0;
     redo[wave] = 0;
   }
   barrier();
@@ -750,29 +845,26 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     lo = min(lo, ranges[0][i]);
     hi = max(hi, ranges[1][i]);
   }
-  cut(w, lo, hi, &k0, &k1);
+  cut(w, uniform(lo), uniform(hi), &k0, &k1);
   const int steps = (k1 - k0 + kStep - 1) / kStep;
-  // row blocks with any row: a tile's rows are its first
-  const uint32_t rows = min(p.tile_tokens, q.rows - w.tile * p.tile_tokens) * p.tile_heads;
-  const int blocks = __builtin_amdgcn_readfirstlane((rows + 31) / 32);
 
-  s16x8 qf[KD / 16];
+  s16x8 qf[kN];
 #pragma unroll
-  for (int s = 0; s < KD / 16; ++s) {
+  for (int s = 0; s < kN; ++s) {
     qf[s] = s16x8{};
     if (t.real)
       qf[s] = *reinterpret_cast<const s16x8*>(p.q + (q.first + t.i) * p.q_token + t.head * p.q_head + s * 32 + half * 16);
   }
-  f32x16 o[4][4];
+  f32x16 o[kBlocks][4];
 #pragma unroll
-  for (int b = 0; b < 4; ++b)
+  for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
     for (int d = 0; d < 4; ++d) o[b][d] = f32x16{};
   float m = -__builtin_inff(), l = 0;
   const ScoreMods mods = score_mods(p);
 
   const uint32_t tiles_at = lds_at(&tiles[0][0]), weights_at = lds_at(&weights[0][0][0][0]);
-  auto load_step = [&](int buf, int slot) {
+  auto load_step = [&](int buf, int slot) BSR_INLINE {
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
       const uint32_t u = (wave * kLoads + n) * 64 + lane, r = u / kUnits, c = u - r * kUnits;
@@ -781,7 +873,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     }
   };
   KeyLoad next{};
-  auto put_offsets = [&](int step) {  // by wave 0, lanes 0..31
+  auto put_offsets = [&](int step) BSR_INLINE {  // by wave 0, lanes 0..31
     int64_t off;
     const bool ok = key_offset(p, next, &off);
     if (lane < kStep) offsets[step & 1][lane] = off;
@@ -797,25 +889,35 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   for (int e = 0; e < 2; ++e)
     v_at[e] = (v_row + 8 * e) * kRowBytes + wave * 256 + ((v_unit ^ unit_swap<64>(v_row + 8 * e)) * 16) + (lane & 1) * 8;
 
-  auto score_step = [&](int step, int buf) {
-    const int j0 = k0 + step * kStep;
-    if (!active) return;
-    f32x16 s[1] = {}, s1 = {};
+  // products of the wave's rows with 32 keys; reads of LDS run kAhead products ahead
+  auto score = [&](int buf, f32x16& s) BSR_INLINE {
     const uint32_t at = tiles_at + buf * kTileBytes + k_at;
-#pragma unroll
-    for (int n = 0; n < KD / 16; n += 2) {
+    auto k_row = [&](int n) BSR_INLINE {
       const uint32_t c = 2 * n + half;
-      s[0] = mfma<T>(lds_row16(at + ((c & ~7u) * 16) + (((c ^ k_swap) & 7) * 16)), qf[n], s[0]);
-      const uint32_t c1 = c + 2;
-      s1 = mfma<T>(lds_row16(at + ((c1 & ~7u) * 16) + (((c1 ^ k_swap) & 7) * 16)), qf[n + 1], s1);
+      return lds_row16(at + (((c ^ k_swap) & 7) * 16) + (c & ~7u) * 16);
+    };
+    s16x8 kf[kAhead];
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) kf[n] = k_row(n);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      if (n == 0) mfma_first<T>(s, kf[0], qf[0]);
+      else mfma_next<T>(s, kf[n % kAhead], qf[n]);
+      if (n + kAhead < kN) kf[n % kAhead] = k_row(n + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    s[0] += s1;
-    float unit = mods.unit;
+    mfma_done(s);
+  };
+  // their scores, what the rows see of them, and the running maximum
+  auto settle = [&](int step, f32x16 (&s)[1], float* unit) BSR_INLINE {
+    const int j0 = k0 + step * kStep;
+    *unit = mods.unit;
     if (kMods) {
-      unit = 1;
+      *unit = 1;
       modify(mods, t.slope2, t.see.pos, j0 + 4 * half, s[0]);
     }
-    const uint32_t bad = outside[step & 3];
+    const uint32_t bad = uniform(outside[step & 3]);
     if (j0 < open_lo || j0 + kStep > open_hi || bad || j0 + kStep > k1) {
       uint64_t see = bit_range(t.see.lo - j0, min(t.see.hi, k1) - j0) & ~static_cast<uint64_t>(bad);
       if (p.tree && t.real) see &= tree_bits(p, t.see.mask, j0 - q.base);
@@ -825,41 +927,45 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
         if (!(see >> (8 * (e / 4) + e % 4) & 1)) s[0][e] = -__builtin_inff();
     }
     float back;
-    const bool rise = weigh<1>(s, unit, m, l, &back);
+    const bool rise = raise<1>(s, *unit, m, l, &back);
+    if (rise && half == 0) backs[step & 1][row] = back;
+    if (lane == 0) rises[step & 1][wave] = rise;
+  };
+  auto leave_weights = [&](int step, f32x16& s, float unit) BSR_INLINE {
+    l += weigh(s, unit, m > -__builtin_inff() ? m : 0.0f);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       float x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = s[0][8 * n + e];
-      *(BSR_LDS s16x8*)(uintptr_t)(weights_at + (((step & 1) * 4 + wave) * 2 + n) * 1024 + lane * 16) = to_half<T>(x);
+      for (int e = 0; e < 8; ++e) x[e] = s[8 * n + e];
+      *(BSR_LDS s16x8*)(uintptr_t)(weights_at + (((step & 1) * kBlocks + wave) * 2 + n) * 1024 + lane * 16) = to_half<T>(x);
     }
-    if (half == 0) backs[step & 1][row] = back;
-    if (lane == 0) rises[step & 1][wave] = rise;
   };
-  auto value_step = [&](int step, int buf) {
-    s16x8 v[2][4];
+  auto rescale = [&](int step) BSR_INLINE {
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int b = 0; b < kBlocks; ++b)
+      if (uniform(rises[step & 1][b])) {
+        const float back = backs[step & 1][b * 32 + col];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) scale_accumulators(o[b][d], back);
+      }
+  };
+  auto values = [&](int step, int buf) BSR_INLINE {
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      s16x8 v[4];
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         const uint32_t at = tiles_at + buf * kTileBytes + 16 * n * kRowBytes;
         const s16x4 a = lds_columns(at + (v_at[0] ^ ((d & 1) * 64)) + (d >> 1) * 128);
         const s16x4 b = lds_columns(at + (v_at[1] ^ ((d & 1) * 64)) + (d >> 1) * 128);
-        v[n][d] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        v[d] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
       }
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      if (b >= blocks) break;
-      if (rises[step & 1][b]) {
-        const float back = backs[step & 1][b * 32 + col];
+      for (int b = 0; b < kBlocks; ++b) {
+        const s16x8 pf = lds_row16(weights_at + (((step & 1) * kBlocks + b) * 2 + n) * 1024 + lane * 16);
 #pragma unroll
-        for (int d = 0; d < 4; ++d) o[b][d] *= back;
-      }
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const s16x8 pf = lds_row16(weights_at + (((step & 1) * 4 + b) * 2 + n) * 1024 + lane * 16);
-#pragma unroll
-        for (int d = 0; d < 4; ++d) o[b][d] = mfma<T>(v[n][d], pf, o[b][d]);
+        for (int d = 0; d < 4; ++d) o[b][d] = mfma<T>(v[d], pf, o[b][d]);
       }
     }
   };
@@ -883,61 +989,76 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
       put_offsets(2);
       if (steps > 3) next = key_load(p, q, k0 + 3 * kStep + lane, k1 - 1);
     }
-    score_step(0, 0);
+    if (scores) {
+      f32x16 s[1];
+      float unit;
+      score(0, s[0]);
+      settle(0, s, &unit);
+      leave_weights(0, s[0], unit);
+    }
   }
   int buf = 0;
-  for (int step = 0; step < steps; ++step) {
+  for (int step = 0; step + 1 < steps; ++step) {
     loads_done();
     barrier();  // step + 1 lies in LDS, the weights of this step too; the buffer of step - 1 is free
     const int buf1 = buf == 2 ? 0 : buf + 1, buf2 = buf1 == 2 ? 0 : buf1 + 1;
     if (wave == 0 && step + 3 < steps) put_offsets(step + 3);
     if (step + 2 < steps) load_step(buf2, step & 1);
     if (wave == 0 && step + 4 < steps) next = key_load(p, q, k0 + (step + 4) * kStep + lane, k1 - 1);
-    if (step + 1 < steps) score_step(step + 1, buf1);
-    value_step(step, buf);
+    if (scores) {
+      f32x16 s[1];
+      float unit;
+      score(buf1, s[0]);
+      settle(step + 1, s, &unit);
+      leave_weights(step + 1, s[0], unit);
+    }
+    rescale(step);
+    values(step, buf);
     buf = buf1;
+  }
+  if (steps > 0) {
+    barrier();
+    rescale(steps - 1);
+    values(steps - 1, buf);
   }
 
   const Sink sink{w.n_splits > 1, w.slot + w.split};
-  l += other_half(l);
-  if (half == 0) {
+  l = sum_halves(l);
+  if (scores && half == 0) {
     stats[0][row] = m;
     stats[1][row] = l;
   }
   barrier();
-  uint32_t bad_rows = 0;  // of the wave's values, by row block, found before any of them is stored
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    if (b >= blocks) break;
+  for (int b = 0; b < kBlocks; ++b) {
     const float lb = stats[1][b * 32 + col];
     const float inv = sink.part ? 1.0f : lb == 0 ? 0.0f : 1.0f / lb;
-    float zero = lb * 0.0f;
+    float zero = lb * 0.0f;  // NaN where a result is not finite
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
       o[b][d] *= inv;
 #pragma unroll
       for (int e = 0; e < 16; ++e) zero += o[b][d][e] * 0.0f;
     }
-    zero += other_half(zero);
-    bad_rows = static_cast<uint32_t>(__ballot(!(zero == 0)));
-    if (lane == 0 && bad_rows) atomicOr(&redo[b], bad_rows);
+    const uint32_t odd = static_cast<uint32_t>(__ballot(!(sum_halves(zero) == 0)));
+    if (lane == 0 && odd) atomicOr(&redo[b], odd);
   }
   barrier();
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    if (b >= blocks) break;
-    const TileRows tb = tile_row(p, q, w, b * 32 + col);
+  for (int b = 0; b < kBlocks; ++b) {
+    const uint32_t at = b * 32 + col;
+    const TileRows tb = tile_row(p, q, w, at);
     if (!tb.real || (redo[b] >> col & 1)) continue;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        put4<T>(p, q, tb, sink, b * 32 + col, 128 * wave + 32 * d + 8 * e + 4 * half,
+        put4<T>(p, q, tb, sink, at, 128 * wave + 32 * d + 8 * e + 4 * half,
                 f32x4{o[b][d][4 * e], o[b][d][4 * e + 1], o[b][d][4 * e + 2], o[b][d][4 * e + 3]});
-    if (half == 0 && wave == 0) put_stats(p, q, tb, sink, b * 32 + col, stats[0][b * 32 + col], stats[1][b * 32 + col]);
+    if (half == 0 && wave == 0) put_stats(p, q, tb, sink, at, stats[0][at], stats[1][at]);
   }
-  for (int b = 0; b < blocks; ++b)
-    for (uint32_t left = redo[b]; left; left &= left - 1) {
+  for (int b = 0; b < kBlocks; ++b)
+    for (uint32_t left = uniform(redo[b]); left; left &= left - 1) {
       const uint32_t c = __builtin_ctz(left);
       if ((c & 3) == static_cast<uint32_t>(wave)) redo_row<T, KD, VD>(p, q, w, sink, b * 32 + c, k0, k1);
     }
@@ -959,19 +1080,19 @@ __global__ __launch_bounds__(kJoinThreads) void k_attend_join(AttnParams p, uint
   for (uint32_t row = blockIdx.y * rows_per + threadIdx.x / kVecs; row < (blockIdx.y + 1) * rows_per; row += kSide) {
     const TileRows t = tile_row(p, q, w, row);
     if (!t.real) continue;
-    const float* ml = p.part_ml + (static_cast<uint64_t>(w.slot) * kTileRows + row) * 2;
-    const float* part = p.part + (static_cast<uint64_t>(w.slot) * kTileRows + row) * VD + d;
+    const float* ml = p.part_ml + (static_cast<uint64_t>(w.slot) * p.tile_rows + row) * 2;
+    const float* part = p.part + (static_cast<uint64_t>(w.slot) * p.tile_rows + row) * VD + d;
     float m = -__builtin_inff();
-    for (uint32_t s = 0; s < w.n_splits; ++s) m = fmaxf(m, ml[s * kTileRows * 2]);
+    for (uint32_t s = 0; s < w.n_splits; ++s) m = fmaxf(m, ml[s * p.tile_rows * 2]);
     const float from = m > -__builtin_inff() ? m : 0.0f;
     float l = 0;
     f32x4 x{};
     for (uint32_t s = 0; s < w.n_splits; ++s) {
-      const float ls = ml[s * kTileRows * 2 + 1];
+      const float ls = ml[s * p.tile_rows * 2 + 1];
       if (ls == 0) continue;
-      const float f = exp2_(ml[s * kTileRows * 2] - from);
+      const float f = exp2_(ml[s * p.tile_rows * 2] - from);
       l += f * ls;
-      x += f * *reinterpret_cast<const f32x4*>(part + static_cast<uint64_t>(s) * kTileRows * VD);
+      x += f * *reinterpret_cast<const f32x4*>(part + static_cast<uint64_t>(s) * p.tile_rows * VD);
     }
     const Sink sink{false, 0};
     x *= l == 0 ? 0.0f : 1.0f / l;
@@ -996,7 +1117,9 @@ hipError_t launch_tiles(const AttnParams& p, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(t.base + p.target)), block(kAttnThreads);
   if (p.k_dim == 64) hipLaunchKernelGGL((k_attend_heads<T, 64, kMods>), grid, block, 0, s, p);
   else if (p.k_dim == 128) hipLaunchKernelGGL((k_attend_heads<T, 128, kMods>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((k_attend_latent<T, kMods>), grid, block, 0, s, p);
+  else if (p.tile_rows == 32) hipLaunchKernelGGL((k_attend_latent<T, kMods, 1>), grid, block, 0, s, p);
+  else if (p.tile_rows == 64) hipLaunchKernelGGL((k_attend_latent<T, kMods, 2>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((k_attend_latent<T, kMods, 4>), grid, block, 0, s, p);
   if (hipError_t e = hipGetLastError()) return e;
   if (!p.target) return hipSuccess;
   const uint32_t base = static_cast<uint32_t>(t.base);
@@ -1010,8 +1133,13 @@ AttnTiling attn_tiling(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
   AttnTiling t{};
   const uint32_t per_kv = n_heads / n_kv_heads;
   t.tile_heads = per_kv < kTileRows ? per_kv : kTileRows;
-  t.tile_tokens = kTileRows / t.tile_heads;
-  t.units = n_kv_heads * ((per_kv + kTileRows - 1) / kTileRows);
+  t.tile_rows = kTileRows;
+  if (v_dim == 512 && n_requests) {  // as few row blocks as an average request's rows need
+    const uint64_t rows = (static_cast<uint64_t>(n_tokens) + n_requests - 1) / n_requests * t.tile_heads;
+    t.tile_rows = rows <= 32 ? 32 : rows <= 64 ? 64 : kTileRows;
+  }
+  t.tile_tokens = t.tile_rows / t.tile_heads;
+  t.units = n_kv_heads * ((per_kv + t.tile_heads - 1) / t.tile_heads);
   // every request may end a tile early; none has a tile without a token
   const uint64_t tiles = (n_tokens / t.tile_tokens) + static_cast<uint64_t>(n_requests < n_tokens ? n_requests : n_tokens);
   t.base = tiles * t.units;
@@ -1019,7 +1147,7 @@ AttnTiling attn_tiling(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
     t.target = v_dim == 512 ? 256 : 512;  // workgroups that the GPU holds at once
     const uint64_t most = t.base * ((max_len + kMinPart - 1) / kMinPart);
     t.slots = most < 2ull * t.target ? most : 2ull * t.target;
-    t.workspace = t.slots * kTileRows * (v_dim + 2) * sizeof(float);
+    t.workspace = t.slots * t.tile_rows * (v_dim + 2) * sizeof(float);
   }
   return t;
 }

@@ -150,12 +150,13 @@ int attend(const bsr_ctx* c, const bsr_attn_args* a, bsr::AttnParams* p, void* s
     return refuse(BSR_E_ARG, "workspace is NULL, not 16-byte aligned or smaller than %llu bytes",
                   static_cast<unsigned long long>(t.workspace));
   if (t.base + t.target >= (1ull << 24)) return refuse(BSR_E_ARG, "too many rows and heads for one launch");
+  p->tile_rows = t.tile_rows;
   p->tile_heads = t.tile_heads;
   p->tile_tokens = t.tile_tokens;
   p->units = t.units;
   p->target = t.target;
   p->part = static_cast<float*>(a->workspace);
-  p->part_ml = p->part + t.slots * bsr::kTileRows * a->v_dim;
+  p->part_ml = p->part + t.slots * t.tile_rows * a->v_dim;
   return enqueue(c, "attention", [&] { return bsr::launch_attention(*p, static_cast<hipStream_t>(stream)); });
 }
 

@@ -83,21 +83,22 @@ struct AttnParams {
   float scale, softcap;
   FastDiv div_block;      // by block_tokens
   // the tiling (attn_tiling)
-  uint32_t tile_heads;    // query heads of a KV head that a tile takes: min(its heads, kTileRows)
-  uint32_t tile_tokens;   // tokens of a tile: kTileRows / tile_heads
+  uint32_t tile_rows;     // query rows of a tile
+  uint32_t tile_heads;    // query heads of a KV head that a tile takes: min(its heads, tile_rows)
+  uint32_t tile_tokens;   // tokens of a tile: tile_rows / tile_heads
   uint32_t units;         // tiles beside one another of the same tokens: KV heads x chunks of their heads
   uint32_t target;        // parts that the batch's key ranges are cut into, about; 0: never cut
-  float* part;            // workspace: sums of parts [slot][kTileRows][v_dim], then their (maximum, sum)
+  float* part;            // workspace: sums of parts [slot][tile_rows][v_dim], then their (maximum, sum)
   float* part_ml;
 };
 
-// An attention tile is kTileRows query rows (tokens x heads of one KV head).
+// An attention tile is up to kTileRows query rows (tokens x heads of one KV head).
 constexpr uint32_t kTileRows = 128;
 // Key ranges are cut into parts of at least this many keys.
 constexpr uint32_t kMinPart = 256;
 
 struct AttnTiling {
-  uint32_t tile_heads, tile_tokens, units, target;
+  uint32_t tile_rows, tile_heads, tile_tokens, units, target;
   uint64_t base;      // tiles x units of the batch, at most
   uint64_t slots;     // partial results, at most
   uint64_t workspace; // bytes
