@@ -159,95 +159,113 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
   return static_cast<uint64_t>(uniform(static_cast<uint32_t>(x >> 32))) << 32 | uniform(static_cast<uint32_t>(x));
 }
 
+// A lane's value from another lane of its row of 16, or from the last lane of
+// the rows before, 0 where there is none; an inclusive sum over the wave of them.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+  return __builtin_amdgcn_update_dpp(0, static_cast<int>(x), kCtrl, kRows, 0xf, false);
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x += dpp<0x111, 0xf>(x);
+  x += dpp<0x112, 0xf>(x);
+  x += dpp<0x114, 0xf>(x);
+  x += dpp<0x118, 0xf>(x);
+  x += dpp<0x142, 0xa>(x);
+  x += dpp<0x143, 0xc>(x);
+  return x;
+}
+__device__ __forceinline__ float wave_total(float x) {
+  const auto add = [](float v, uint32_t u) { return v + __uint_as_float(u); };
+  x = add(x, dpp<0x111, 0xf>(__float_as_uint(x)));
+  x = add(x, dpp<0x112, 0xf>(__float_as_uint(x)));
+  x = add(x, dpp<0x114, 0xf>(__float_as_uint(x)));
+  x = add(x, dpp<0x118, 0xf>(__float_as_uint(x)));
+  x = add(x, dpp<0x142, 0xa>(__float_as_uint(x)));
+  x = add(x, dpp<0x143, 0xc>(__float_as_uint(x)));
+  return __shfl(x, 63);
+}
+
+// What a lane knows of its request: tiles of tokens, and the keys that one of
+// them can see at most.
 struct RequestWork {
-  uint32_t tiles, range;  // tiles of tokens, keys that one of them can see at most
+  Request q;
+  uint32_t tiles, range;
 };
 
 __device__ __forceinline__ RequestWork request_work(const AttnParams& p, uint32_t r) {
-  RequestWork w{0, 0};
+  RequestWork w{};
   if (r >= p.n_requests) return w;
-  const Request q = request_of(p, r);
-  w.tiles = (q.rows + p.tile_tokens - 1) / p.tile_tokens;
-  w.range = q.n;
-  if (p.window && !p.prefix) w.range = min(w.range, p.window + (p.tree ? q.rows : min(static_cast<uint32_t>(q.rows), p.tile_tokens)));
+  w.q = request_of(p, r);
+  const uint32_t rows = w.q.rows;
+  w.tiles = (rows + p.tile_tokens - 1) / p.tile_tokens;
+  w.range = w.q.n;
+  if (p.window && !p.prefix) w.range = min(w.range, p.window + (p.tree ? rows : min(rows, p.tile_tokens)));
   return w;
 }
 
 __device__ __forceinline__ uint32_t splits_of(uint32_t range, uint32_t part) { return range > part ? (range + part - 1) / part : 1; }
 
-__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) {
-  const uint32_t lo = __shfl_up(static_cast<uint32_t>(v), d), hi = __shfl_up(static_cast<uint32_t>(v >> 32), d);
-  return static_cast<uint64_t>(hi) << 32 | lo;
-}
-__device__ __forceinline__ uint64_t shfl64(uint64_t v, int l) {
-  const uint32_t lo = __shfl(static_cast<uint32_t>(v), l), hi = __shfl(static_cast<uint32_t>(v >> 32), l);
-  return static_cast<uint64_t>(hi) << 32 | lo;
-}
-
-// Keys of a part: the batch's (tile, key) pairs over the target, so that the
-// parts come out alike whatever the requests' lengths.  Parts of ranges that are cut
-// at all number at most 2 x target (each range is longer than a part).
-__device__ __forceinline__ uint32_t part_keys(const AttnParams& p) {
+// Keys of a part, from the batch's (tile, key) pairs: their share of the
+// target, so that the parts come out alike whatever the requests' lengths.  Parts of ranges that
+// are cut at all number at most 2 x target (each range is longer than a
+// part), and all items at most target more than there are tiles; a sum of up to 2^20
+// positive numbers in fp32 is off by less than the tenth that is added.
+__device__ __forceinline__ uint32_t part_keys(const AttnParams& p, const RequestWork& first) {
   if (!p.target) return 0x7fffffffu;
   const uint32_t lane = threadIdx.x & 63;
-  uint64_t total = 0;
-  for (uint32_t r0 = 0; r0 < p.n_requests; r0 += 64) {
+  float total = static_cast<float>(first.tiles) * static_cast<float>(first.range);
+  for (uint32_t r0 = 64; r0 < p.n_requests; r0 += 64) {
     const RequestWork w = request_work(p, r0 + lane);
-    total += static_cast<uint64_t>(w.tiles) * w.range;
+    total += static_cast<float>(w.tiles) * static_cast<float>(w.range);
   }
-  if (p.n_requests > 1) {
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint64_t u = shfl_up64(total, d);
-      if (static_cast<int>(lane) >= d) total += u;
-    }
-    total = shfl64(total, 63);
-  } else {
-    total = shfl64(total, 0);
-  }
-  const uint64_t part = (total * p.units + p.target - 1) / p.target;
-  if (part >= 0x7fffff00u) return 0x7fffffffu;
-  const uint32_t k = static_cast<uint32_t>(part);
-  return uniform(((k > kMinPart ? k : kMinPart) + 63) & ~63u);
+  total = p.n_requests > 1 ? wave_total(total) : __shfl(total, 0);
+  const float part = total * static_cast<float>(p.units) * 1.1f / static_cast<float>(p.target);
+  if (!(part < 1e9f)) return 0x7fffffffu;
+  const uint32_t k = static_cast<uint32_t>(part) + 1;
+  return uniform(((k > p.min_part ? k : p.min_part) + 63) & ~63u);
 }
 
 // Item `b` of the batch (every wave finds it for itself); kBase: b counts tiles
 // x units, and the item is its first part.
 template <bool kBase>
-__device__ __forceinline__ bool find_work(const AttnParams& p, uint32_t b, Work* out) {
-  const uint32_t lane = threadIdx.x & 63, part = part_keys(p);
+__device__ __forceinline__ bool find_work(const AttnParams& p, uint32_t b, Work* out, Request* q) {
+  const uint32_t lane = threadIdx.x & 63;
+  RequestWork w = request_work(p, lane);
+  const uint32_t part = part_keys(p, w);
   uint32_t items_before = 0, slots_before = 0;
   for (uint32_t r0 = 0; r0 < p.n_requests; r0 += 64) {
-    const RequestWork w = request_work(p, r0 + lane);
+    if (r0) w = request_work(p, r0 + lane);
     const uint32_t s = splits_of(w.range, part), base = w.tiles * p.units;
     const uint32_t items = kBase ? base : base * s, slots = s > 1 ? base * s : 0;
     uint32_t ends = items, slot_ends = slots;
-    if (p.n_requests > 1)
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t u = __shfl_up(ends, d), v = __shfl_up(slot_ends, d);
-        if (static_cast<int>(lane) >= d) {
-          ends += u;
-          slot_ends += v;
-        }
-      }
+    if (p.n_requests > 1) {
+      ends = wave_scan(ends);
+      slot_ends = wave_scan(slot_ends);
+    }
     ends += items_before;
     slot_ends += slots_before;
     const uint64_t past = __ballot(ends > b);
     if (past) {
       const int l = __builtin_ctzll(past);
-      const uint32_t local = uniform(b - (__shfl(ends, l) - __shfl(items, l)));
+      const auto of = [&](uint32_t x) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(x), l)); };
+      const uint32_t local = b - of(ends - items);
       out->r = r0 + l;
-      out->n_splits = uniform(__shfl(s, l));
-      const uint32_t tiles = uniform(__shfl(w.tiles, l));
+      out->n_splits = of(s);
       const uint32_t rest = kBase ? local : local / out->n_splits;
       out->split = kBase ? 0 : local - rest * out->n_splits;
       const uint32_t t = rest / p.units;
       out->unit = rest - t * p.units;
-      out->tile = tiles - 1 - t;  // the last tokens see the most keys: first
-      out->slot = uniform(__shfl(slot_ends, l) - __shfl(slots, l)) + rest * out->n_splits;
+      out->tile = of(w.tiles) - 1 - t;  // the last tokens see the most keys: first
+      out->slot = of(slot_ends - slots) + rest * out->n_splits;
+      q->first = of(w.q.first);
+      q->rows = of(w.q.rows);
+      q->n = of(w.q.n);
+      q->base = q->n - q->rows;
+      q->table = p.tables + static_cast<uint64_t>(out->r) * p.table_stride;
       return true;
     }
-    items_before = __shfl(ends, 63);
-    slots_before = __shfl(slot_ends, 63);
+    items_before = __builtin_amdgcn_readlane(ends, 63);
+    slots_before = __builtin_amdgcn_readlane(slot_ends, 63);
   }
   return false;
 }
@@ -427,6 +445,7 @@ __device__ __forceinline__ int wave_max(int x) {
 // Scores (times log2(e)) of a lane's keys j0 + 8 (e / 4) + e % 4, j0 = the
 // first key of the 32 plus 4 h, from their products.  Without cap and bias the products stay as they
 // are, and `unit` (scale x log2(e)) goes into the exponent.
+constexpr int kCap = 1, kSlopes = 2;  // what is done to a score
 struct ScoreMods {
   float unit;       // scale x log2(e)
   float cap2;       // softcap x log2(e), 0 without
@@ -441,13 +460,15 @@ __device__ __forceinline__ ScoreMods score_mods(const AttnParams& p) {
   return m;
 }
 
+template <int kMods>
 __device__ __forceinline__ void modify(const ScoreMods& m, float slope2, int pos, int j0, f32x16& s) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
     float x = s[e];
-    if (m.cap2 > 0) x = m.cap2 - 2 * m.cap2 * __builtin_amdgcn_rcpf(exp2_(x * m.in_cap) + 1);
+    if (kMods & kCap) x = m.cap2 - 2 * m.cap2 * __builtin_amdgcn_rcpf(exp2_(x * m.in_cap) + 1);
     else x *= m.unit;
-    s[e] = x - slope2 * static_cast<float>(abs(pos - (j0 + 8 * (e / 4) + e % 4)));
+    if (kMods & kSlopes) x = __builtin_fmaf(-slope2, fabsf(static_cast<float>(pos - (j0 + 8 * (e / 4) + e % 4))), x);
+    s[e] = x;
   }
 }
 
@@ -535,6 +556,22 @@ __device__ void redo_row(const AttnParams& p, const Request& q, const Work& w, c
   if ((threadIdx.x & 63) == 0) put_stats(p, q, t, k, row, m, l);
 }
 
+// Keys [lo, hi) that a tile's rows see any of; documents are looked at by the
+// caller.
+__device__ __forceinline__ void tile_range(const AttnParams& p, const Request& q, const Work& w, int* lo, int* hi) {
+  const int i0 = w.tile * p.tile_tokens, i1 = min(i0 + static_cast<int>(p.tile_tokens), q.rows);
+  *lo = 0;
+  if (p.tree) {
+    *hi = q.n;
+    if (p.window) *lo = max(0, q.base - static_cast<int>(p.window));  // a row that sees no row stands at base - 1
+  } else {
+    *hi = q.base + i1;
+    if (p.prefix) *hi = max(*hi, min(p.prefix[w.r], q.n));
+    *hi = max(*hi, 0);
+    if (p.window) *lo = max(0, q.base + i0 - static_cast<int>(p.window) + 1);
+  }
+}
+
 // Part `split` of the keys [lo, hi): whole steps of 64 keys.
 __device__ __forceinline__ void cut(const Work& w, int lo, int hi, int* k0, int* k1) {
   if (hi < lo) hi = lo;
@@ -588,19 +625,18 @@ __device__ __forceinline__ uint32_t unit_swap(uint32_t row) {
   return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
 }
 
-template <typename T, int D, bool kMods>
-__global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) {
+template <typename T, int D, int kMods>
+__global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(AttnParams p) {
   constexpr int kStep = 64, kUnits = D / 8, kTileBytes = kStep * D * 2;
   constexpr int kRowsPerLoad = 64 / kUnits, kLoads = kStep / 4 / kRowsPerLoad;  // per wave, K and V each
   __shared__ __attribute__((aligned(1024))) uint8_t kv_tiles[2][2][kTileBytes];
   __shared__ int64_t offsets[2][kStep];
   __shared__ uint64_t outside[4];
-  __shared__ int ranges[2][4];
-  __shared__ uint32_t redo[4];
+  __shared__ int ranges[4];
 
   Work w;
-  if (!find_work<false>(p, blockIdx.x, &w)) return;
-  const Request q = request_of(p, w.r);
+  Request q;
+  if (!find_work<false>(p, blockIdx.x, &w, &q)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
   const uint32_t kv = w.unit / (p.units / p.n_kv_heads);
@@ -610,19 +646,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
   // keys that all of the wave's rows see without a look at their masks
   const int open_lo = uniform(wave_max(t.real ? t.see.lo : 0));
   const int open_hi = uniform(wave_min(!t.real ? 0x7fffffff : p.tree ? min(t.see.hi, q.base) : t.see.hi));
-  const int wave_lo = uniform(wave_min(t.see.lo)), wave_hi = uniform(wave_max(t.see.hi));
-  if (lane == 0) {
-    ranges[0][wave] = wave_lo;
-    ranges[1][wave] = wave_hi;
-    redo[wave] = 0;
+  const int wave_lo = wave_min(t.see.lo);
+  int lo, hi, k0, k1;
+  tile_range(p, q, w, &lo, &hi);
+  if (p.documents) {  // a tile of late documents starts late
+    if (lane == 0) ranges[wave] = wave_lo;
+    barrier();
+    lo = uniform(max(lo, min(min(ranges[0], ranges[1]), min(ranges[2], ranges[3]))));
   }
-  barrier();
-  int lo = ranges[0][0], hi = ranges[1][0], k0, k1;
-  for (int i = 1; i < 4; ++i) {
-    lo = min(lo, ranges[0][i]);
-    hi = max(hi, ranges[1][i]);
-  }
-  cut(w, uniform(lo), uniform(hi), &k0, &k1);
+  cut(w, lo, hi, &k0, &k1);
   const int steps = (k1 - k0 + kStep - 1) / kStep;
 
   s16x8 qf[D / 16];
@@ -654,24 +686,22 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
     }
   };
   KeyLoad next{};
-  auto put_offsets = [&](int step) BSR_INLINE {  // by wave 0
+  auto put_offsets = [&](int step, const KeyLoad& k) BSR_INLINE {  // by wave 0
     int64_t off;
-    const bool ok = key_offset(p, next, &off);
+    const bool ok = key_offset(p, k, &off);
     offsets[step & 1][lane] = off;
     const uint64_t bad = ~__ballot(ok);
     if (lane == 0) outside[step & 3] = bad;
   };
-
   if (steps > 0) {
-    if (wave == 0) {
-      next = key_load(p, q, k0 + lane, k1 - 1);
-      put_offsets(0);
-      if (steps > 1) next = key_load(p, q, k0 + kStep + lane, k1 - 1);
+    if (wave == 0) {  // (steps past the last read its last key's block id)
+      const KeyLoad k_first = key_load(p, q, k0 + lane, k1 - 1), k_second = key_load(p, q, k0 + kStep + lane, k1 - 1);
+      next = key_load(p, q, k0 + 2 * kStep + lane, k1 - 1);
+      put_offsets(0, k_first);
+      put_offsets(1, k_second);
     }
     barrier();
-    if (wave == 0 && steps > 1) put_offsets(1);
     load_step(0, 0);
-    if (wave == 0 && steps > 2) next = key_load(p, q, k0 + 2 * kStep + lane, k1 - 1);
   }
 
   // read positions: K, row col of 32; V transposed, row 4 h + (lane % 16) / 4
@@ -683,17 +713,24 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
   for (int e = 0; e < 2; ++e)
     v_at[e] = (v_row + 8 * e) * (D * 2) + ((v_unit ^ unit_swap<D>(v_row + 8 * e)) * 16) + (lane & 1) * 8;
 
-  for (int step = 0; step < steps; ++step) {
+  // waits for a step, and sends the loads of the next
+  auto turn = [&](int step) BSR_INLINE {
     loads_done();
     barrier();
     const int buf = step & 1;
-    if (wave == 0 && step + 2 < steps) put_offsets(step + 2);
+    if (wave == 0 && step + 2 < steps) put_offsets(step + 2, next);
     if (step + 1 < steps) load_step(buf ^ 1, buf ^ 1);
     if (wave == 0 && step + 3 < steps) next = key_load(p, q, k0 + (step + 3) * kStep + lane, k1 - 1);
-    const int j0 = k0 + step * kStep;
-    if (!active || j0 + kStep <= wave_lo || j0 >= wave_hi) continue;
+  };
+  // a wave without rows loads its share all the same (in a loop of its own: a
+  // way round the sums' products would have them copied at every step)
+  if (!active)
+    for (int step = 0; step < steps; ++step) turn(step);
+  else
+  for (int step = 0; step < steps; ++step) {
+    turn(step);
+    const int buf = step & 1, j0 = k0 + step * kStep;
     const uint32_t k_tile = tiles_at + buf * (2 * kTileBytes), v_tile = k_tile + kTileBytes;
-
     constexpr int kN = D / 16, kD = D / 32;
     auto k_row = [&](int u, int n) BSR_INLINE {
       return lds_row16(k_tile + u * 32 * (D * 2) + k_at + (((2 * n + half) ^ k_swap) * 16));
@@ -704,37 +741,36 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
       const s16x4 a = lds_columns(at + (v_at[0] ^ (d * 64))), b = lds_columns(at + (v_at[1] ^ (d * 64)));
       return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    // reads of LDS run ahead of the products: of the second 32 keys while the
-    // first are multiplied, of the first values before the softmax
+    // reads of LDS run kAhead products ahead, into the registers that a product has
+    // just left; the first values are read before the softmax
+    constexpr int kAhead = 4;
     f32x16 s[2] = {};
-    s16x8 kf[kN], vf[2][kD];
+    s16x8 kf[kAhead], vf[kD];
 #pragma unroll
-    for (int n = 0; n < kN; ++n) kf[n] = k_row(0, n);
+    for (int i = 0; i < kAhead; ++i) kf[i] = k_row(0, i);
 #pragma unroll
-    for (int n = 0; n < kN; ++n) {
-      s[0] = mfma<T>(kf[n], qf[n], s[0]);
-      kf[n] = k_row(1, n);
+    for (int i = 0; i < 2 * kN; ++i) {
+      s[i / kN] = mfma<T>(kf[i % kAhead], qf[i % kN], s[i / kN]);
+      if (i + kAhead < 2 * kN) kf[i % kAhead] = k_row((i + kAhead) / kN, (i + kAhead) % kN);
     }
 #pragma unroll
-    for (int n = 0; n < kN; ++n) s[1] = mfma<T>(kf[n], qf[n], s[1]);
+    for (int d = 0; d < kD; ++d) vf[d] = v_cols(0, d);
+    BSR_ORDER(kLdsRead, kAhead);
 #pragma unroll
-    for (int d = 0; d < kD; ++d) vf[0][d] = v_cols(0, d);
-    BSR_ORDER(kLdsRead, kN);
-#pragma unroll
-    for (int n = 0; n < kN; ++n) {
+    for (int i = 0; i < 2 * kN - kAhead; ++i) {
       BSR_ORDER(kMatrix, 1);
       BSR_ORDER(kLdsRead, 1);
     }
 #pragma unroll
-    for (int n = 0; n < kN; ++n) {
+    for (int i = 0; i < kAhead; ++i) {
       BSR_ORDER(kMatrix, 1);
-      BSR_ORDER(kLdsRead, 1);
+      BSR_ORDER(kLdsRead, 2);
     }
     float unit = mods.unit;
     if (kMods) {
       unit = 1;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) modify(mods, t.slope2, t.see.pos, j0 + 32 * u + 4 * half, s[u]);
+      for (int u = 0; u < 2; ++u) modify<kMods>(mods, t.slope2, t.see.pos, j0 + 32 * u + 4 * half, s[u]);
     }
     const uint64_t bad = uniform(outside[step & 3]);
     if (j0 < open_lo || j0 + kStep > open_hi || bad || j0 + kStep > k1) {
@@ -754,21 +790,16 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
     }
     const float from = m > -__builtin_inff() ? m : 0.0f;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      l += weigh(s[u], unit, from);
+    for (int g = 0; g < 4; ++g) {  // 16 keys each
+      if (g % 2 == 0) l += weigh(s[g / 2], unit, from);
+      float x[8];
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int g = 2 * u + n;
-        if (g < 3) {
+      for (int e = 0; e < 8; ++e) x[e] = s[g / 2][8 * (g % 2) + e];
+      const s16x8 pf = to_half<T>(x);
 #pragma unroll
-          for (int d = 0; d < kD; ++d) vf[(g + 1) & 1][d] = v_cols(g + 1, d);
-        }
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = s[u][8 * n + e];
-        const s16x8 pf = to_half<T>(x);
-#pragma unroll
-        for (int d = 0; d < kD; ++d) o[d] = mfma<T>(vf[g & 1][d], pf, o[d]);
+      for (int d = 0; d < kD; ++d) {
+        o[d] = mfma<T>(vf[d], pf, o[d]);
+        if (g < 3) vf[d] = v_cols(g + 1, d);
       }
     }
   }
@@ -807,7 +838,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void k_attend_heads(AttnParams p) 
 // of step t + 1 and values of step t share a stretch between two barriers, and
 // step t + 2 is loaded meanwhile.
 // ---------------------------------------------------------------------------
-template <typename T, bool kMods, int kBlocks>
+template <typename T, int kMods, int kBlocks>
 __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThreads, 1) void k_attend_latent(AttnParams p) {
   constexpr int KD = 576, VD = 512, kStep = 32, kUnits = KD / 8, kRowBytes = KD * 2, kTileBytes = kStep * kRowBytes;
   constexpr int kBufs = 3, kLoads = kStep * kUnits / kAttnThreads;  // 9 per wave
@@ -819,12 +850,12 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   __shared__ float stats[2][32 * kBlocks];
   __shared__ int64_t offsets[2][kStep];
   __shared__ uint32_t outside[4];
-  __shared__ int ranges[2][4];
+  __shared__ int ranges[4];
   __shared__ uint32_t redo[4];
 
   Work w;
-  if (!find_work<false>(p, blockIdx.x, &w)) return;
-  const Request q = request_of(p, w.r);
+  Request q;
+  if (!find_work<false>(p, blockIdx.x, &w, &q)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
   const bool scores = wave < kBlocks;  // waves with query rows of their own
@@ -832,20 +863,19 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   const TileRows t = tile_row(p, q, w, row);
   const int open_lo = uniform(wave_max(t.real ? t.see.lo : 0));
   const int open_hi = uniform(wave_min(!t.real ? 0x7fffffff : p.tree ? min(t.see.hi, q.base) : t.see.hi));
-  const int wave_lo = uniform(wave_min(t.see.lo)), wave_hi = uniform(wave_max(t.see.hi));
+  const int wave_lo = wave_min(t.see.lo);
   if (lane == 0) {
-    ranges[0][wave] = wave_lo;
-    ranges[1][wave] = wave_hi;
     rises[0][wave] = rises[1][wave] = 0;
     redo[wave] = 0;
   }
-  barrier();
-  int lo = ranges[0][0], hi = ranges[1][0], k0, k1;
-  for (int i = 1; i < 4; ++i) {
-    lo = min(lo, ranges[0][i]);
-    hi = max(hi, ranges[1][i]);
+  int lo, hi, k0, k1;
+  tile_range(p, q, w, &lo, &hi);
+  if (p.documents) {  // a tile of late documents starts late
+    if (lane == 0) ranges[wave] = wave_lo;
+    barrier();
+    lo = uniform(max(lo, min(min(ranges[0], ranges[1]), min(ranges[2], ranges[3]))));
   }
-  cut(w, uniform(lo), uniform(hi), &k0, &k1);
+  cut(w, lo, hi, &k0, &k1);
   const int steps = (k1 - k0 + kStep - 1) / kStep;
 
   s16x8 qf[kN];
@@ -873,9 +903,9 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     }
   };
   KeyLoad next{};
-  auto put_offsets = [&](int step) BSR_INLINE {  // by wave 0, lanes 0..31
+  auto put_offsets = [&](int step, const KeyLoad& k) BSR_INLINE {  // by wave 0, lanes 0..31
     int64_t off;
-    const bool ok = key_offset(p, next, &off);
+    const bool ok = key_offset(p, k, &off);
     if (lane < kStep) offsets[step & 1][lane] = off;
     const uint32_t bad = ~static_cast<uint32_t>(__ballot(ok));
     if (lane == 0) outside[step & 3] = bad;
@@ -915,7 +945,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     *unit = mods.unit;
     if (kMods) {
       *unit = 1;
-      modify(mods, t.slope2, t.see.pos, j0 + 4 * half, s[0]);
+      modify<kMods>(mods, t.slope2, t.see.pos, j0 + 4 * half, s[0]);
     }
     const uint32_t bad = uniform(outside[step & 3]);
     if (j0 < open_lo || j0 + kStep > open_hi || bad || j0 + kStep > k1) {
@@ -971,24 +1001,20 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   };
 
   if (steps > 0) {
-    if (wave == 0) {
-      next = key_load(p, q, k0 + lane, k1 - 1);
-      put_offsets(0);
-      if (steps > 1) {
-        next = key_load(p, q, k0 + kStep + lane, k1 - 1);
-        put_offsets(1);
-      }
-      if (steps > 2) next = key_load(p, q, k0 + 2 * kStep + lane, k1 - 1);
+    KeyLoad k_third{};
+    if (wave == 0) {  // (steps past the last read its last key's block id)
+      const KeyLoad k_first = key_load(p, q, k0 + lane, k1 - 1), k_second = key_load(p, q, k0 + kStep + lane, k1 - 1);
+      k_third = key_load(p, q, k0 + 2 * kStep + lane, k1 - 1);
+      next = key_load(p, q, k0 + 3 * kStep + lane, k1 - 1);
+      put_offsets(0, k_first);
+      put_offsets(1, k_second);
     }
     barrier();
     load_step(0, 0);
     if (steps > 1) load_step(1, 1);
     loads_done();
     barrier();
-    if (wave == 0 && steps > 2) {
-      put_offsets(2);
-      if (steps > 3) next = key_load(p, q, k0 + 3 * kStep + lane, k1 - 1);
-    }
+    if (wave == 0 && steps > 2) put_offsets(2, k_third);
     if (scores) {
       f32x16 s[1];
       float unit;
@@ -1002,7 +1028,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     loads_done();
     barrier();  // step + 1 lies in LDS, the weights of this step too; the buffer of step - 1 is free
     const int buf1 = buf == 2 ? 0 : buf + 1, buf2 = buf1 == 2 ? 0 : buf1 + 1;
-    if (wave == 0 && step + 3 < steps) put_offsets(step + 3);
+    if (wave == 0 && step + 3 < steps) put_offsets(step + 3, next);
     if (step + 2 < steps) load_step(buf2, step & 1);
     if (wave == 0 && step + 4 < steps) next = key_load(p, q, k0 + (step + 4) * kStep + lane, k1 - 1);
     if (scores) {
@@ -1069,35 +1095,51 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
 // joined them, always in the order of the parts.
 // ---------------------------------------------------------------------------
 constexpr int kJoinThreads = 128;
+constexpr uint32_t kJoinParts = 512;  // parts whose weights lie in LDS at once
 
+// A workgroup joins rows that its threads hold four dimensions each of: a row
+// of 512, or several of fewer.  The parts' weights come first; their sums are then read
+// several at a time.
 template <typename T, int VD>
 __global__ __launch_bounds__(kJoinThreads) void k_attend_join(AttnParams p, uint32_t rows_per) {
-  constexpr int kVecs = VD / 4, kSide = kJoinThreads / kVecs;  // threads of a row; rows side by side
+  constexpr uint32_t kVecs = VD / 4, kSide = kJoinThreads / kVecs;  // threads of a row; rows side by side
+  __shared__ float weight[kSide][kJoinParts];
   Work w;
-  if (!find_work<true>(p, blockIdx.x, &w) || w.n_splits < 2) return;
-  const Request q = request_of(p, w.r);
-  const uint32_t d = threadIdx.x % kVecs * 4;
-  for (uint32_t row = blockIdx.y * rows_per + threadIdx.x / kVecs; row < (blockIdx.y + 1) * rows_per; row += kSide) {
+  Request q;
+  if (!find_work<true>(p, blockIdx.x, &w, &q) || w.n_splits < 2) return;
+  const uint32_t side = threadIdx.x / kVecs, at = threadIdx.x % kVecs;
+  const uint32_t part_rows = p.tile_rows;
+  for (uint32_t r0 = blockIdx.y * rows_per; r0 < (blockIdx.y + 1) * rows_per; r0 += kSide) {
+    const uint32_t row = r0 + side;
     const TileRows t = tile_row(p, q, w, row);
-    if (!t.real) continue;
-    const float* ml = p.part_ml + (static_cast<uint64_t>(w.slot) * p.tile_rows + row) * 2;
-    const float* part = p.part + (static_cast<uint64_t>(w.slot) * p.tile_rows + row) * VD + d;
-    float m = -__builtin_inff();
-    for (uint32_t s = 0; s < w.n_splits; ++s) m = fmaxf(m, ml[s * p.tile_rows * 2]);
+    const float* ml = p.part_ml + (static_cast<uint64_t>(w.slot) * part_rows + row) * 2;
+    const float* part = p.part + (static_cast<uint64_t>(w.slot) * part_rows + row) * VD + at * 4;
+    float m = -__builtin_inff(), l = 0;
+    if (t.real)
+      for (uint32_t s = 0; s < w.n_splits; ++s) m = fmaxf(m, ml[s * part_rows * 2]);
     const float from = m > -__builtin_inff() ? m : 0.0f;
-    float l = 0;
     f32x4 x{};
-    for (uint32_t s = 0; s < w.n_splits; ++s) {
-      const float ls = ml[s * p.tile_rows * 2 + 1];
-      if (ls == 0) continue;
-      const float f = exp2_(ml[s * p.tile_rows * 2] - from);
-      l += f * ls;
-      x += f * *reinterpret_cast<const f32x4*>(part + static_cast<uint64_t>(s) * p.tile_rows * VD);
+    for (uint32_t s0 = 0; s0 < w.n_splits; s0 += kJoinParts) {
+      const uint32_t n = min(kJoinParts, w.n_splits - s0);
+      __syncthreads();
+      if (t.real)
+        for (uint32_t s = at; s < n; s += kVecs) {
+          const float ls = ml[(s0 + s) * part_rows * 2 + 1];
+          // a part without a seen key weighs nothing, whatever its sums hold
+          weight[side][s] = ls == 0 ? 0.0f : exp2_(ml[(s0 + s) * part_rows * 2] - from);
+        }
+      __syncthreads();
+      if (!t.real) continue;
+      for (uint32_t s = 0; s < n; ++s) l += weight[side][s] * ml[(s0 + s) * part_rows * 2 + 1];
+#pragma unroll 8
+      for (uint32_t s = 0; s < n; ++s)
+        x += weight[side][s] * *reinterpret_cast<const f32x4*>(part + static_cast<uint64_t>(s0 + s) * part_rows * VD);
     }
+    if (!t.real) continue;
     const Sink sink{false, 0};
     x *= l == 0 ? 0.0f : 1.0f / l;
-    put4<T>(p, q, t, sink, row, d, x);
-    if (d == 0) put_stats(p, q, t, sink, row, m, l);
+    put4<T>(p, q, t, sink, row, at * 4, x);
+    if (at == 0) put_stats(p, q, t, sink, row, m, l);
   }
 }
 
@@ -1111,7 +1153,7 @@ hipError_t launch_join(const AttnParams& p, uint32_t base, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, bool kMods>
+template <typename T, int kMods>
 hipError_t launch_tiles(const AttnParams& p, hipStream_t s) {
   const AttnTiling t = attn_tiling(p.n_requests, p.n_tokens, p.n_heads, p.n_kv_heads, p.v_dim, p.max_len);
   const dim3 grid(static_cast<uint32_t>(t.base + p.target)), block(kAttnThreads);
@@ -1124,6 +1166,12 @@ hipError_t launch_tiles(const AttnParams& p, hipStream_t s) {
   if (!p.target) return hipSuccess;
   const uint32_t base = static_cast<uint32_t>(t.base);
   return p.v_dim == 64 ? launch_join<T, 64>(p, base, s) : p.v_dim == 128 ? launch_join<T, 128>(p, base, s) : launch_join<T, 512>(p, base, s);
+}
+
+template <typename T>
+hipError_t launch_typed(const AttnParams& p, hipStream_t s) {
+  if (p.softcap > 0) return p.slopes ? launch_tiles<T, kCap | kSlopes>(p, s) : launch_tiles<T, kCap>(p, s);
+  return p.slopes ? launch_tiles<T, kSlopes>(p, s) : launch_tiles<T, 0>(p, s);
 }
 
 }  // namespace
@@ -1143,9 +1191,10 @@ AttnTiling attn_tiling(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
   // every request may end a tile early; none has a tile without a token
   const uint64_t tiles = (n_tokens / t.tile_tokens) + static_cast<uint64_t>(n_requests < n_tokens ? n_requests : n_tokens);
   t.base = tiles * t.units;
-  if (max_len > kMinPart) {
+  t.min_part = v_dim == 512 ? 64 : 128;
+  if (max_len > t.min_part) {
     t.target = v_dim == 512 ? 256 : 512;  // workgroups that the GPU holds at once
-    const uint64_t most = t.base * ((max_len + kMinPart - 1) / kMinPart);
+    const uint64_t most = t.base * ((max_len + t.min_part - 1) / t.min_part);
     t.slots = most < 2ull * t.target ? most : 2ull * t.target;
     t.workspace = t.slots * t.tile_rows * (v_dim + 2) * sizeof(float);
   }
@@ -1153,9 +1202,7 @@ AttnTiling attn_tiling(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
 }
 
 hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
-  const bool mods = p.softcap > 0 || p.slopes;
-  if (p.f16) return mods ? launch_tiles<_Float16, true>(p, s) : launch_tiles<_Float16, false>(p, s);
-  return mods ? launch_tiles<__bf16, true>(p, s) : launch_tiles<__bf16, false>(p, s);
+  return p.f16 ? launch_typed<_Float16>(p, s) : launch_typed<__bf16>(p, s);
 }
 
 }  // namespace bsr

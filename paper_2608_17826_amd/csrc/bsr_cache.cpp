@@ -155,6 +155,7 @@ int attend(const bsr_ctx* c, const bsr_attn_args* a, bsr::AttnParams* p, void* s
   p->tile_tokens = t.tile_tokens;
   p->units = t.units;
   p->target = t.target;
+  p->min_part = t.min_part;
   p->part = static_cast<float*>(a->workspace);
   p->part_ml = p->part + t.slots * t.tile_rows * a->v_dim;
   return enqueue(c, "attention", [&] { return bsr::launch_attention(*p, static_cast<hipStream_t>(stream)); });

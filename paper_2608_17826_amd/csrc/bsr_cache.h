@@ -88,17 +88,16 @@ struct AttnParams {
   uint32_t tile_tokens;   // tokens of a tile: tile_rows / tile_heads
   uint32_t units;         // tiles beside one another of the same tokens: KV heads x chunks of their heads
   uint32_t target;        // parts that the batch's key ranges are cut into, about; 0: never cut
+  uint32_t min_part;      // keys of a part, at least
   float* part;            // workspace: sums of parts [slot][tile_rows][v_dim], then their (maximum, sum)
   float* part_ml;
 };
 
 // An attention tile is up to kTileRows query rows (tokens x heads of one KV head).
 constexpr uint32_t kTileRows = 128;
-// Key ranges are cut into parts of at least this many keys.
-constexpr uint32_t kMinPart = 256;
 
 struct AttnTiling {
-  uint32_t tile_rows, tile_heads, tile_tokens, units, target;
+  uint32_t tile_rows, tile_heads, tile_tokens, units, target, min_part;
   uint64_t base;      // tiles x units of the batch, at most
   uint64_t slots;     // partial results, at most
   uint64_t workspace; // bytes
