@@ -346,7 +346,20 @@ __device__ __forceinline__ uint32_t lds_at(const void* p) {
 __device__ __forceinline__ void load_to_lds(const uint8_t* src, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory");
 }
-__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// The same from a scalar address and a lane's offset (a vector instruction
+// that wrote the address, unseen by the compiler to be followed by a load, is five wait states back).
+__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+// 64 lanes x 4 bytes likewise.
+__device__ __forceinline__ void load_words_to_lds(const void* src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory");
+}
+// Waits until at most `left` of the wave's loads are under way (they end in order).
+template <int left = 0>
+__device__ __forceinline__ void loads_done() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(left) : "memory");
+}
 __device__ __forceinline__ void barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
   __builtin_amdgcn_s_barrier();
@@ -840,16 +853,22 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
 // ---------------------------------------------------------------------------
 template <typename T, int kMods, int kBlocks>
 __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThreads, 1) void k_attend_latent(AttnParams p) {
-  constexpr int KD = 576, VD = 512, kStep = 32, kUnits = KD / 8, kRowBytes = KD * 2, kTileBytes = kStep * kRowBytes;
-  constexpr int kBufs = 3, kLoads = kStep * kUnits / kAttnThreads;  // 9 per wave
+  constexpr int KD = 576, VD = 512, kStep = 32, kTileBytes = kStep * KD * 2;
+  // LDS of a step: the eight records of each wave, their values (1,024 bytes
+  // each) and then the rest of their keys (128 bytes each), so that a load of 64 lanes takes a record's
+  // values, at a scalar address, or the rest of all eight
+  constexpr int kValueBytes = VD * 2, kRestBytes = (KD - VD) * 2, kWaveBytes = kTileBytes / 4;
+  // steps loaded or in use at once: three where there is LDS for no more
+  constexpr int kBufs = kBlocks == 4 ? 3 : 4, kLoads = 9;  // of a wave and step
+  constexpr int kKeys = kStep / 4, kIdSteps = 64 / kKeys;  // keys that a wave loads at a step; steps of one load of block ids
   constexpr int kN = KD / 16, kAhead = 6;
   __shared__ __attribute__((aligned(1024))) uint8_t tiles[kBufs][kTileBytes];
   __shared__ __attribute__((aligned(16))) uint8_t weights[2][kBlocks][2][1024];  // [step][rows / 32][16 keys][lane]
   __shared__ float backs[2][32 * kBlocks];
   __shared__ uint32_t rises[2][4];
   __shared__ float stats[2][32 * kBlocks];
-  __shared__ int64_t offsets[2][kStep];
-  __shared__ uint32_t outside[4];
+  __shared__ int32_t block_ids[4][2][64];
+  __shared__ __attribute__((aligned(4))) uint8_t outside[8][4];
   __shared__ int ranges[4];
   __shared__ uint32_t redo[4];
 
@@ -894,37 +913,63 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   const ScoreMods mods = score_mods(p);
 
   const uint32_t tiles_at = lds_at(&tiles[0][0]), weights_at = lds_at(&weights[0][0][0][0]);
-  auto load_step = [&](int buf, int slot) BSR_INLINE {
-#pragma unroll
-    for (int n = 0; n < kLoads; ++n) {
-      const uint32_t u = (wave * kLoads + n) * 64 + lane, r = u / kUnits, c = u - r * kUnits;
-      const uint32_t from = (c & ~7u) | ((c ^ unit_swap<64>(r)) & 7);
-      load_to_lds(p.k_pool + offsets[slot][r] + from * 16, tiles_at + buf * kTileBytes + (wave * kLoads + n) * 1024);
+  // A wave loads keys 8 wave .. 8 wave + 7 of a step, and their block ids
+  // kIdSteps steps at a time: it waits for its own loads alone.
+  auto key_at = [&](int step, int key) BSR_INLINE { return min(k0 + step * kStep + wave * kKeys + key, k1 - 1); };
+  auto load_ids = [&](int first_step) BSR_INLINE {
+    const int j = key_at(first_step + lane / kKeys, lane % kKeys);
+    load_words_to_lds(q.table + p.div_block.div(j), lds_at(&block_ids[wave][first_step / kIdSteps & 1][0]));
+  };
+  // the offset of the lane's record, key lane % 8 of a step: its block id is read some time before
+  int32_t id = 0;
+  int64_t offset = 0;
+  auto read_id = [&](int step) BSR_INLINE {
+    id = block_ids[wave][step / kIdSteps & 1][step % kIdSteps * kKeys + lane % kKeys];
+  };
+  auto find_offset = [&](int step) BSR_INLINE {
+    const int j = key_at(step, lane % kKeys);
+    const KeyLoad k{j, p.div_block.div(j), id};
+    const bool ok = key_offset(p, k, &offset);
+    const uint64_t bad = ~__ballot(ok);
+    if (lane == 0) outside[step & 7][wave] = static_cast<uint8_t>(bad);
+  };
+  // load n of a step: the values of record n, or the rest of all; units of 16
+  // bytes are permuted by the record's row
+  auto load_unit = [&](int n, int buf) BSR_INLINE {
+    const uint32_t to = tiles_at + buf * kTileBytes + wave * kWaveBytes + n * 1024;
+    const uint32_t lo = static_cast<uint32_t>(offset), hi = static_cast<uint32_t>(offset >> 32);
+    if (n < kKeys) {
+      const uint64_t off = static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(hi, n))) << 32 |
+                           static_cast<uint32_t>(__builtin_amdgcn_readlane(lo, n));
+      load_to_lds(p.k_pool + off, (lane ^ unit_swap<128>(wave * kKeys + n)) * 16, to);
+    } else {
+      const int r = lane >> 3;
+      const uint64_t off = static_cast<uint64_t>(__shfl(hi, r)) << 32 | __shfl(lo, r);
+      load_to_lds(p.k_pool + off + kValueBytes + (((lane & 7) ^ unit_swap<64>(wave * kKeys + r)) * 16), to);
     }
   };
-  KeyLoad next{};
-  auto put_offsets = [&](int step, const KeyLoad& k) BSR_INLINE {  // by wave 0, lanes 0..31
-    int64_t off;
-    const bool ok = key_offset(p, k, &off);
-    if (lane < kStep) offsets[step & 1][lane] = off;
-    const uint32_t bad = ~static_cast<uint32_t>(__ballot(ok));
-    if (lane == 0) outside[step & 3] = bad;
+  auto load_step = [&](int buf) BSR_INLINE {
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) load_unit(n, buf);
   };
 
-  const uint32_t k_at = col * kRowBytes, k_swap = unit_swap<64>(col);
+  // read positions: the key of row col, 8 dimensions of it; four values of row
+  // 4 h + (lane % 16) / 4, transposed
+  const uint32_t k_at = (col >> 3) * kWaveBytes + (col & 7) * kValueBytes + ((half ^ unit_swap<128>(col)) * 16);
+  const uint32_t k_rest = (col >> 3) * kWaveBytes + kKeys * kValueBytes + (col & 7) * kRestBytes + ((half ^ unit_swap<64>(col)) * 16);
   const uint32_t v_row = 4 * half + ((lane & 15) >> 2);
   const uint32_t v_unit = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
   uint32_t v_at[2];
 #pragma unroll
   for (int e = 0; e < 2; ++e)
-    v_at[e] = (v_row + 8 * e) * kRowBytes + wave * 256 + ((v_unit ^ unit_swap<64>(v_row + 8 * e)) * 16) + (lane & 1) * 8;
+    v_at[e] = e * kWaveBytes + v_row * kValueBytes + wave * 256 + ((v_unit ^ unit_swap<128>(v_row + 8 * e)) * 16) + (lane & 1) * 8;
 
   // products of the wave's rows with 32 keys; reads of LDS run kAhead products ahead
-  auto score = [&](int buf, f32x16& s) BSR_INLINE {
-    const uint32_t at = tiles_at + buf * kTileBytes + k_at;
+  // (`between` goes on beside them)
+  auto score = [&](int buf, f32x16& s, auto between) BSR_INLINE {
+    const uint32_t at = tiles_at + buf * kTileBytes;
     auto k_row = [&](int n) BSR_INLINE {
-      const uint32_t c = 2 * n + half;
-      return lds_row16(at + (((c ^ k_swap) & 7) * 16) + (c & ~7u) * 16);
+      return n < VD / 16 ? lds_row16(at + (k_at ^ (n % 8 * 32)) + n / 8 * 256) : lds_row16(at + (k_rest ^ ((n - VD / 16) * 32)));
     };
     s16x8 kf[kAhead];
 #pragma unroll
@@ -935,6 +980,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
       if (n == 0) mfma_first<T>(s, kf[0], qf[0]);
       else mfma_next<T>(s, kf[n % kAhead], qf[n]);
       if (n + kAhead < kN) kf[n % kAhead] = k_row(n + kAhead);
+      between(n);
       __builtin_amdgcn_sched_barrier(0);
     }
     mfma_done(s);
@@ -947,7 +993,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
       *unit = 1;
       modify<kMods>(mods, t.slope2, t.see.pos, j0 + 4 * half, s[0]);
     }
-    const uint32_t bad = uniform(outside[step & 3]);
+    const uint32_t bad = uniform(*reinterpret_cast<const uint32_t*>(&outside[step & 7][0]));
     if (j0 < open_lo || j0 + kStep > open_hi || bad || j0 + kStep > k1) {
       uint64_t see = bit_range(t.see.lo - j0, min(t.see.hi, k1) - j0) & ~static_cast<uint64_t>(bad);
       if (p.tree && t.real) see &= tree_bits(p, t.see.mask, j0 - q.base);
@@ -986,9 +1032,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
       s16x8 v[4];
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
-        const uint32_t at = tiles_at + buf * kTileBytes + 16 * n * kRowBytes;
-        const s16x4 a = lds_columns(at + (v_at[0] ^ ((d & 1) * 64)) + (d >> 1) * 128);
-        const s16x4 b = lds_columns(at + (v_at[1] ^ ((d & 1) * 64)) + (d >> 1) * 128);
+        const uint32_t at = tiles_at + buf * kTileBytes + 2 * n * kWaveBytes;
+        const s16x4 a = lds_columns(at + (v_at[0] ^ (d * 64))), b = lds_columns(at + (v_at[1] ^ (d * 64)));
         v[d] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
       }
 #pragma unroll
@@ -1001,42 +1046,50 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   };
 
   if (steps > 0) {
-    KeyLoad k_third{};
-    if (wave == 0) {  // (steps past the last read its last key's block id)
-      const KeyLoad k_first = key_load(p, q, k0 + lane, k1 - 1), k_second = key_load(p, q, k0 + kStep + lane, k1 - 1);
-      k_third = key_load(p, q, k0 + 2 * kStep + lane, k1 - 1);
-      next = key_load(p, q, k0 + 3 * kStep + lane, k1 - 1);
-      put_offsets(0, k_first);
-      put_offsets(1, k_second);
-    }
-    barrier();
-    load_step(0, 0);
-    if (steps > 1) load_step(1, 1);
+    load_ids(0);
     loads_done();
+    if (steps > kIdSteps) load_ids(kIdSteps);
+#pragma unroll
+    for (int i = 0; i < kBufs; ++i) {
+      read_id(i);
+      find_offset(i);
+      if (i < kBufs - 1 && i < steps) load_step(i);
+    }
+    if (steps < kBufs - 1) loads_done();
+    else loads_done<(kBufs - 2) * kLoads>();
     barrier();
-    if (wave == 0 && steps > 2) put_offsets(2, k_third);
     if (scores) {
       f32x16 s[1];
       float unit;
-      score(0, s[0]);
+      score(0, s[0], [](int) {});
       settle(0, s, &unit);
       leave_weights(0, s[0], unit);
     }
   }
   int buf = 0;
   for (int step = 0; step + 1 < steps; ++step) {
-    loads_done();
-    barrier();  // step + 1 lies in LDS, the weights of this step too; the buffer of step - 1 is free
-    const int buf1 = buf == 2 ? 0 : buf + 1, buf2 = buf1 == 2 ? 0 : buf1 + 1;
-    if (wave == 0 && step + 3 < steps) put_offsets(step + 3, next);
-    if (step + 2 < steps) load_step(buf2, step & 1);
-    if (wave == 0 && step + 4 < steps) next = key_load(p, q, k0 + (step + 4) * kStep + lane, k1 - 1);
+    // step + 1 lies in LDS, and so do the weights of this step; the buffer of step - 1 is free
+    if (kBufs > 3 && step + kBufs - 2 < steps) loads_done<(kBufs - 3) * kLoads>();  // later steps' loads go on
+    else loads_done();
+    barrier();
+    const int buf1 = buf + 1 == kBufs ? 0 : buf + 1, last = buf == 0 ? kBufs - 1 : buf - 1;
+    if (step % kIdSteps == 0 && step && step + kIdSteps < steps) load_ids(step + kIdSteps);
+    const bool more = step + kBufs - 1 < steps;
+    const int ahead = step + kBufs;  // its ids are read whether there is such a step or not (keys end at the last)
     if (scores) {
       f32x16 s[1];
       float unit;
-      score(buf1, s[0]);
+      score(buf1, s[0], [&](int n) BSR_INLINE {
+        if (n < kLoads && more) load_unit(n, last);
+        if (n == 16) read_id(ahead);
+        if (n == 24) find_offset(ahead);
+      });
       settle(step + 1, s, &unit);
       leave_weights(step + 1, s[0], unit);
+    } else {
+      if (more) load_step(last);
+      read_id(ahead);
+      find_offset(ahead);
     }
     rescale(step);
     values(step, buf);
@@ -1095,51 +1148,61 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
 // joined them, always in the order of the parts.
 // ---------------------------------------------------------------------------
 constexpr int kJoinThreads = 128;
-constexpr uint32_t kJoinParts = 512;  // parts whose weights lie in LDS at once
+// Parts of a range, at most: a part is at least 1.1 / target of the whole batch's keys.
+constexpr uint32_t kJoinParts = 512;
+static_assert(kMaxTarget / 1.1 + 2 < kJoinParts, "a range's parts fit");
 
-// A workgroup joins rows that its threads hold four dimensions each of: a row
-// of 512, or several of fewer.  The parts' weights come first; their sums are then read
-// several at a time.
+// A workgroup joins rows that its threads hold four dimensions each of: one of
+// 512, or several of fewer.  The first sums are read beside the maxima, the others eight at a time.
 template <typename T, int VD>
 __global__ __launch_bounds__(kJoinThreads) void k_attend_join(AttnParams p, uint32_t rows_per) {
   constexpr uint32_t kVecs = VD / 4, kSide = kJoinThreads / kVecs;  // threads of a row; rows side by side
-  __shared__ float weight[kSide][kJoinParts];
+  constexpr uint32_t kFirst = 8;
+  __shared__ float part_m[kSide][kJoinParts], part_l[kSide][kJoinParts];
   Work w;
   Request q;
   if (!find_work<true>(p, blockIdx.x, &w, &q) || w.n_splits < 2) return;
-  const uint32_t side = threadIdx.x / kVecs, at = threadIdx.x % kVecs;
-  const uint32_t part_rows = p.tile_rows;
+  const uint32_t side = threadIdx.x / kVecs, at = threadIdx.x % kVecs, n = w.n_splits;
+  const uint64_t step = static_cast<uint64_t>(p.tile_rows) * VD;
   for (uint32_t r0 = blockIdx.y * rows_per; r0 < (blockIdx.y + 1) * rows_per; r0 += kSide) {
     const uint32_t row = r0 + side;
     const TileRows t = tile_row(p, q, w, row);
-    const float* ml = p.part_ml + (static_cast<uint64_t>(w.slot) * part_rows + row) * 2;
-    const float* part = p.part + (static_cast<uint64_t>(w.slot) * part_rows + row) * VD + at * 4;
-    float m = -__builtin_inff(), l = 0;
-    if (t.real)
-      for (uint32_t s = 0; s < w.n_splits; ++s) m = fmaxf(m, ml[s * part_rows * 2]);
-    const float from = m > -__builtin_inff() ? m : 0.0f;
-    f32x4 x{};
-    for (uint32_t s0 = 0; s0 < w.n_splits; s0 += kJoinParts) {
-      const uint32_t n = min(kJoinParts, w.n_splits - s0);
-      __syncthreads();
-      if (t.real)
-        for (uint32_t s = at; s < n; s += kVecs) {
-          const float ls = ml[(s0 + s) * part_rows * 2 + 1];
-          // a part without a seen key weighs nothing, whatever its sums hold
-          weight[side][s] = ls == 0 ? 0.0f : exp2_(ml[(s0 + s) * part_rows * 2] - from);
-        }
-      __syncthreads();
-      if (!t.real) continue;
-      for (uint32_t s = 0; s < n; ++s) l += weight[side][s] * ml[(s0 + s) * part_rows * 2 + 1];
-#pragma unroll 8
-      for (uint32_t s = 0; s < n; ++s)
-        x += weight[side][s] * *reinterpret_cast<const f32x4*>(part + static_cast<uint64_t>(s0 + s) * part_rows * VD);
+    const float* ml = p.part_ml + (static_cast<uint64_t>(w.slot) * p.tile_rows + row) * 2;
+    const float* part = p.part + (static_cast<uint64_t>(w.slot) * p.tile_rows + row) * VD + at * 4;
+    f32x4 first[kFirst];
+    if (t.real) {
+#pragma unroll
+      for (uint32_t s = 0; s < kFirst; ++s) first[s] = *reinterpret_cast<const f32x4*>(part + min(s, n - 1) * step);
+      for (uint32_t s = at; s < n; s += kVecs) {
+        part_m[side][s] = ml[static_cast<uint64_t>(s) * p.tile_rows * 2];
+        part_l[side][s] = ml[static_cast<uint64_t>(s) * p.tile_rows * 2 + 1];
+      }
     }
-    if (!t.real) continue;
-    const Sink sink{false, 0};
-    x *= l == 0 ? 0.0f : 1.0f / l;
-    put4<T>(p, q, t, sink, row, at * 4, x);
-    if (at == 0) put_stats(p, q, t, sink, row, m, l);
+    __syncthreads();
+    float m = -__builtin_inff(), l = 0;
+    f32x4 x{};
+    if (t.real) {
+#pragma unroll 8
+      for (uint32_t s = 0; s < n; ++s) m = fmaxf(m, part_m[side][s]);
+      const float from = m > -__builtin_inff() ? m : 0.0f;
+      const auto add = [&](uint32_t s, f32x4 sums) BSR_INLINE {
+        const float ls = part_l[side][s];
+        // a part without a seen key weighs nothing
+        const float f = ls == 0 ? 0.0f : exp2_(part_m[side][s] - from);
+        l += f * ls;
+        x += f * sums;
+      };
+#pragma unroll
+      for (uint32_t s = 0; s < kFirst; ++s)
+        if (s < n) add(s, first[s]);
+#pragma unroll 8
+      for (uint32_t s = kFirst; s < n; ++s) add(s, *reinterpret_cast<const f32x4*>(part + s * step));
+      const Sink sink{false, 0};
+      x *= l == 0 ? 0.0f : 1.0f / l;
+      put4<T>(p, q, t, sink, row, at * 4, x);
+      if (at == 0) put_stats(p, q, t, sink, row, m, l);
+    }
+    __syncthreads();
   }
 }
 
@@ -1182,8 +1245,9 @@ AttnTiling attn_tiling(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
   const uint32_t per_kv = n_heads / n_kv_heads;
   t.tile_heads = per_kv < kTileRows ? per_kv : kTileRows;
   t.tile_rows = kTileRows;
-  if (v_dim == 512 && n_requests) {  // as few row blocks as an average request's rows need
-    const uint64_t rows = (static_cast<uint64_t>(n_tokens) + n_requests - 1) / n_requests * t.tile_heads;
+  if (v_dim == 512 && n_requests && n_tokens % n_requests == 0) {
+    // requests of as many rows each, it seems: no more row blocks than those need
+    const uint64_t rows = static_cast<uint64_t>(n_tokens) / n_requests * t.tile_heads;
     t.tile_rows = rows <= 32 ? 32 : rows <= 64 ? 64 : kTileRows;
   }
   t.tile_tokens = t.tile_rows / t.tile_heads;
@@ -1193,7 +1257,7 @@ AttnTiling attn_tiling(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
   t.base = tiles * t.units;
   t.min_part = v_dim == 512 ? 64 : 128;
   if (max_len > t.min_part) {
-    t.target = v_dim == 512 ? 256 : 512;  // workgroups that the GPU holds at once
+    t.target = v_dim == 512 ? 256 : kMaxTarget;  // workgroups that the GPU holds at once
     const uint64_t most = t.base * ((max_len + t.min_part - 1) / t.min_part);
     t.slots = most < 2ull * t.target ? most : 2ull * t.target;
     t.workspace = t.slots * t.tile_rows * (v_dim + 2) * sizeof(float);

@@ -95,6 +95,7 @@ struct AttnParams {
 
 // An attention tile is up to kTileRows query rows (tokens x heads of one KV head).
 constexpr uint32_t kTileRows = 128;
+constexpr uint32_t kMaxTarget = 512;
 
 struct AttnTiling {
   uint32_t tile_rows, tile_heads, tile_tokens, units, target, min_part;
