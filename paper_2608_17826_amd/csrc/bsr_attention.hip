@@ -106,6 +106,7 @@ __device__ void attend_row(const AttnParams& p, const Request& q, const Row& w, 
     if (at >= 0) {
       const T* k = reinterpret_cast<const T*>(p.k_pool + at + kv * (2 * KD));
       float dot = 0;
+#pragma unroll 2
       for (int d = 0; d < KD; d += 8) {
         T x[8];
         __builtin_memcpy(x, __builtin_assume_aligned(k + d, 16), 16);
@@ -205,24 +206,52 @@ __device__ __forceinline__ RequestWork request_work(const AttnParams& p, uint32_
 
 __device__ __forceinline__ uint32_t splits_of(uint32_t range, uint32_t part) { return range > part ? (range + part - 1) / part : 1; }
 
-// Keys of a part, from the batch's (tile, key) pairs: their share of the
-// target, so that the parts come out alike whatever the requests' lengths.  Parts of ranges that
-// are cut at all number at most 2 x target (each range is longer than a
-// part), and all items at most target more than there are tiles; a sum of up to 2^20
-// positive numbers in fp32 is off by less than the tenth that is added.
+__device__ __forceinline__ uint32_t wave_sum(const AttnParams& p, uint32_t x) {  // over the requests of a batch of up to 64
+  return p.n_requests > 1 ? static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(wave_scan(x)), 63)) : uniform(x);
+}
+
+// Keys of a part.  Where the batch has no more tiles x units than the GPU holds
+// workgroups (target), its ranges are cut into as many parts as those, so that all run at
+// once and end together; up to twice as many tiles are cut into twice as many parts; more are
+// left whole.  All parts have the same length, which starts at their share
+// of the batch's (tile, key) pairs and grows until the parts, each range's
+// rounded up, are no more than that.  Past six rounds, and for batches of over 64 requests,
+// it is the length that no rounding makes too many of.
 __device__ __forceinline__ uint32_t part_keys(const AttnParams& p, const RequestWork& first) {
-  if (!p.target) return 0x7fffffffu;
+  constexpr uint32_t kWhole = 0x7fffffffu;
+  if (!p.target) return kWhole;
   const uint32_t lane = threadIdx.x & 63;
+  uint32_t base;
   float total = static_cast<float>(first.tiles) * static_cast<float>(first.range);
-  for (uint32_t r0 = 64; r0 < p.n_requests; r0 += 64) {
-    const RequestWork w = request_work(p, r0 + lane);
-    total += static_cast<float>(w.tiles) * static_cast<float>(w.range);
+  if (p.n_requests <= 64) {
+    base = wave_sum(p, first.tiles) * p.units;
+    total = p.n_requests > 1 ? wave_total(total) : __shfl(total, 0);
+  } else {
+    uint32_t tiles = first.tiles;
+    for (uint32_t r0 = 64; r0 < p.n_requests; r0 += 64) {
+      const RequestWork w = request_work(p, r0 + lane);
+      tiles += w.tiles;
+      total += static_cast<float>(w.tiles) * static_cast<float>(w.range);
+    }
+    base = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(wave_scan(tiles)), 63)) * p.units;
+    total = wave_total(total);
   }
-  total = p.n_requests > 1 ? wave_total(total) : __shfl(total, 0);
-  const float part = total * static_cast<float>(p.units) * 1.1f / static_cast<float>(p.target);
-  if (!(part < 1e9f)) return 0x7fffffffu;
-  const uint32_t k = static_cast<uint32_t>(part) + 1;
-  return uniform(((k > p.min_part ? k : p.min_part) + 63) & ~63u);
+  const uint32_t limit = base <= p.target ? p.target : 2 * p.target;
+  if (base >= limit) return kWhole;
+  total *= static_cast<float>(p.units);
+  const auto length = [&](float keys) {  // whole steps; the sum is off by less than a thousandth (2^14 additions a lane)
+    const uint32_t k = static_cast<uint32_t>(fminf(keys * 1.002f, 2e9f)) + 1;
+    return uniform(((k > p.min_part ? k : p.min_part) + 63) & ~63u);
+  };
+  if (p.n_requests <= 64) {
+    uint32_t part = length(total / static_cast<float>(limit));
+    for (int i = 0; i < 6; ++i) {
+      const uint32_t n = wave_sum(p, first.tiles * splits_of(first.range, part)) * p.units;
+      if (n <= limit) return part;
+      part = length(static_cast<float>(part) * static_cast<float>(n) / static_cast<float>(limit));
+    }
+  }
+  return length(total / static_cast<float>(limit - base));
 }
 
 // Item `b` of the batch (every wave finds it for itself); kBase: b counts tiles
@@ -610,8 +639,10 @@ __device__ __forceinline__ KeyLoad key_load(const AttnParams& p, const Request& 
   return k;
 }
 __device__ __forceinline__ bool key_offset(const AttnParams& p, const KeyLoad& k, int64_t* off) {
-  const bool ok = k.id >= 0 && static_cast<uint32_t>(k.id) < p.pool_blocks;
-  *off = ok ? static_cast<int64_t>(k.id) * p.block_bytes + static_cast<int64_t>(k.j - k.block * p.div_block.d) * p.record_bytes : 0;
+  const bool ok = static_cast<uint32_t>(k.id) < p.pool_blocks;  // (fewer than 2^31)
+  const uint32_t keep = 0u - static_cast<uint32_t>(ok);  // no branch: latent steps do this beside their products
+  const uint32_t id = k.id & keep, at = (k.j - k.block * p.div_block.d) & keep;
+  *off = static_cast<int64_t>(id) * p.block_bytes + at * p.record_bytes;  // a block is smaller than 2^31 bytes
   return ok;
 }
 
@@ -760,11 +791,11 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
     f32x16 s[2] = {};
     s16x8 kf[kAhead], vf[kD];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) kf[i] = k_row(0, i);
+    for (int i = 0; i < kAhead; ++i) kf[i] = k_row(i % 2, i / 2);
 #pragma unroll
-    for (int i = 0; i < 2 * kN; ++i) {
-      s[i / kN] = mfma<T>(kf[i % kAhead], qf[i % kN], s[i / kN]);
-      if (i + kAhead < 2 * kN) kf[i % kAhead] = k_row((i + kAhead) / kN, (i + kAhead) % kN);
+    for (int i = 0; i < 2 * kN; ++i) {  // two sums in turn: a product that goes on with the last one's waits for it
+      s[i % 2] = mfma<T>(kf[i % kAhead], qf[i / 2], s[i % 2]);
+      if (i + kAhead < 2 * kN) kf[i % kAhead] = k_row((i + kAhead) % 2, (i + kAhead) / 2);
     }
 #pragma unroll
     for (int d = 0; d < kD; ++d) vf[d] = v_cols(0, d);
@@ -861,12 +892,17 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   // steps loaded or in use at once: three where there is LDS for no more
   constexpr int kBufs = kBlocks == 4 ? 3 : 4, kLoads = 9;  // of a wave and step
   constexpr int kKeys = kStep / 4, kIdSteps = 64 / kKeys;  // keys that a wave loads at a step; steps of one load of block ids
-  constexpr int kN = KD / 16, kAhead = 6;
+  constexpr int kN = KD / 16, kAhead = 3;
+  constexpr int kHeld = kBlocks == 4 ? 32 : kN;  // products whose queries lie in registers; the others' are read from LDS
+  // A product that goes on with the last one's sum waits for it, twice as long as it takes itself: scores
+  // alternate between two sums, or, where registers are short, with the value products.
+  constexpr int kSums = kBlocks == 4 ? 1 : 2;
   __shared__ __attribute__((aligned(1024))) uint8_t tiles[kBufs][kTileBytes];
   __shared__ __attribute__((aligned(16))) uint8_t weights[2][kBlocks][2][1024];  // [step][rows / 32][16 keys][lane]
   __shared__ float backs[2][32 * kBlocks];
-  __shared__ uint32_t rises[2][4];
+  __shared__ __attribute__((aligned(16))) uint32_t rises[2][4];
   __shared__ float stats[2][32 * kBlocks];
+  __shared__ __attribute__((aligned(16))) uint8_t queries[kBlocks == 4 ? 4 : 1][kN - kHeld + 1][1024];  // [wave][n - kHeld][lane]
   __shared__ int32_t block_ids[4][2][64];
   __shared__ __attribute__((aligned(4))) uint8_t outside[8][4];
   __shared__ int ranges[4];
@@ -877,7 +913,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   if (!find_work<false>(p, blockIdx.x, &w, &q)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const bool scores = wave < kBlocks;  // waves with query rows of their own
+  const bool scores = kBlocks == 4 || wave < kBlocks;  // waves with query rows of their own
   const uint32_t row = wave * 32 + col;
   const TileRows t = tile_row(p, q, w, row);
   const int open_lo = uniform(wave_max(t.real ? t.see.lo : 0));
@@ -897,12 +933,13 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   cut(w, lo, hi, &k0, &k1);
   const int steps = (k1 - k0 + kStep - 1) / kStep;
 
-  s16x8 qf[kN];
+  s16x8 qf[kHeld];
 #pragma unroll
-  for (int s = 0; s < kN; ++s) {
-    qf[s] = s16x8{};
-    if (t.real)
-      qf[s] = *reinterpret_cast<const s16x8*>(p.q + (q.first + t.i) * p.q_token + t.head * p.q_head + s * 32 + half * 16);
+  for (int n = 0; n < kN; ++n) {
+    s16x8 x{};
+    if (t.real) x = *reinterpret_cast<const s16x8*>(p.q + (q.first + t.i) * p.q_token + t.head * p.q_head + n * 32 + half * 16);
+    if (n < kHeld) qf[n] = x;
+    else *reinterpret_cast<s16x8*>(&queries[wave][n - kHeld][lane * 16]) = x;
   }
   f32x16 o[kBlocks][4];
 #pragma unroll
@@ -931,7 +968,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     const KeyLoad k{j, p.div_block.div(j), id};
     const bool ok = key_offset(p, k, &offset);
     const uint64_t bad = ~__ballot(ok);
-    if (lane == 0) outside[step & 7][wave] = static_cast<uint8_t>(bad);
+    // (by every lane: what stands beside the products stays one block of instructions)
+    outside[step & 7][wave] = static_cast<uint8_t>(bad);
   };
   // load n of a step: the values of record n, or the rest of all; units of 16
   // bytes are permuted by the record's row
@@ -964,26 +1002,34 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   for (int e = 0; e < 2; ++e)
     v_at[e] = e * kWaveBytes + v_row * kValueBytes + wave * 256 + ((v_unit ^ unit_swap<128>(v_row + 8 * e)) * 16) + (lane & 1) * 8;
 
-  // products of the wave's rows with 32 keys; reads of LDS run kAhead products ahead
-  // (`between` goes on beside them)
-  auto score = [&](int buf, f32x16& s, auto between) BSR_INLINE {
+  // Products of the wave's rows with the 32 keys in buffer `buf`; `beside(n)` goes on
+  // beside them, the value products of another step among it.  Reads of LDS run kAhead
+  // products ahead; the order is pinned.
+  auto score = [&](int buf, f32x16& s, auto beside) BSR_INLINE {
     const uint32_t at = tiles_at + buf * kTileBytes;
     auto k_row = [&](int n) BSR_INLINE {
       return n < VD / 16 ? lds_row16(at + (k_at ^ (n % 8 * 32)) + n / 8 * 256) : lds_row16(at + (k_rest ^ ((n - VD / 16) * 32)));
     };
-    s16x8 kf[kAhead];
+    s16x8 kf[kAhead], q_next{};
+    f32x16 sums[kSums];
 #pragma unroll
     for (int n = 0; n < kAhead; ++n) kf[n] = k_row(n);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int n = 0; n < kN; ++n) {
-      if (n == 0) mfma_first<T>(s, kf[0], qf[0]);
-      else mfma_next<T>(s, kf[n % kAhead], qf[n]);
+      if (n < kSums) mfma_first<T>(sums[n], kf[n], qf[n]);
+      else mfma_next<T>(sums[n % kSums], kf[n % kAhead], n < kHeld ? qf[n < kHeld ? n : 0] : q_next);
+      if (n + 1 >= kHeld && n + 1 < kN) q_next = *reinterpret_cast<const s16x8*>(&queries[wave][n + 1 - kHeld][lane * 16]);
       if (n + kAhead < kN) kf[n % kAhead] = k_row(n + kAhead);
-      between(n);
+      beside(n);
       __builtin_amdgcn_sched_barrier(0);
     }
-    mfma_done(s);
+    mfma_done(sums[0]);
+    s = sums[0];
+    if (kSums == 2) {
+      mfma_done(sums[kSums - 1]);
+      s += sums[kSums - 1];
+    }
   };
   // their scores, what the rows see of them, and the running maximum
   auto settle = [&](int step, f32x16 (&s)[1], float* unit) BSR_INLINE {
@@ -1018,45 +1064,57 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     }
   };
   auto rescale = [&](int step) BSR_INLINE {
+    const u32x4 rise = *reinterpret_cast<const u32x4*>(&rises[step & 1][0]);
+    if (!uniform(rise[0] | rise[1] | rise[2] | rise[3])) return;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
-      if (uniform(rises[step & 1][b])) {
+      if (uniform(rise[b])) {
         const float back = backs[step & 1][b * 32 + col];
 #pragma unroll
         for (int d = 0; d < 4; ++d) scale_accumulators(o[b][d], back);
       }
   };
+  // The value products of a step, 8 kBlocks of them: 16 keys g, 32 dimensions d, 32 rows b,
+  // the last fastest.  The weights of all rows stay in registers over the dimensions; the values of the next dimensions,
+  // and at the last of them the weights of the next keys, are read ahead.
+  constexpr int kValueProducts = 8 * kBlocks;
+  s16x8 vf[2], pf[kBlocks];
+  auto v_cols = [&](int buf, int g, int d) BSR_INLINE {
+    const uint32_t at = tiles_at + buf * kTileBytes + 2 * g * kWaveBytes;
+    const s16x4 a = lds_columns(at + (v_at[0] ^ (d * 64))), b = lds_columns(at + (v_at[1] ^ (d * 64)));
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto p_cols = [&](int step, int g, int b) BSR_INLINE {
+    return lds_row16(weights_at + (((step & 1) * kBlocks + b) * 2 + g) * 1024 + lane * 16);
+  };
+  auto start_values = [&](int step, int buf) BSR_INLINE {
+    vf[0] = v_cols(buf, 0, 0);
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) pf[b] = p_cols(step, 0, b);
+  };
+  auto value_product = [&](int step, int buf, int i) BSR_INLINE {
+    const int b = i % kBlocks, d = i / kBlocks % 4, g = i / (4 * kBlocks), next = i / kBlocks + 1;
+    if (b == 0 && next < 8) vf[next & 1] = v_cols(buf, next / 4, next % 4);
+    o[b][d] = mfma<T>(vf[d & 1], pf[b], o[b][d]);
+    if (g == 0 && d == 3) pf[b] = p_cols(step, 1, b);
+  };
   auto values = [&](int step, int buf) BSR_INLINE {
+    start_values(step, buf);
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      s16x8 v[4];
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const uint32_t at = tiles_at + buf * kTileBytes + 2 * n * kWaveBytes;
-        const s16x4 a = lds_columns(at + (v_at[0] ^ (d * 64))), b = lds_columns(at + (v_at[1] ^ (d * 64)));
-        v[d] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        const s16x8 pf = lds_row16(weights_at + (((step & 1) * kBlocks + b) * 2 + n) * 1024 + lane * 16);
-#pragma unroll
-        for (int d = 0; d < 4; ++d) o[b][d] = mfma<T>(v[d], pf, o[b][d]);
-      }
-    }
+    for (int i = 0; i < kValueProducts; ++i) value_product(step, buf, i);
   };
 
   if (steps > 0) {
     load_ids(0);
     loads_done();
-    if (steps > kIdSteps) load_ids(kIdSteps);
+    load_ids(kIdSteps);
 #pragma unroll
     for (int i = 0; i < kBufs; ++i) {
       read_id(i);
       find_offset(i);
-      if (i < kBufs - 1 && i < steps) load_step(i);
+      if (i < kBufs - 1) load_step(i);
     }
-    if (steps < kBufs - 1) loads_done();
-    else loads_done<(kBufs - 2) * kLoads>();
+    loads_done<(kBufs - 2) * kLoads>();
     barrier();
     if (scores) {
       f32x16 s[1];
@@ -1066,36 +1124,44 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
       leave_weights(0, s[0], unit);
     }
   }
-  int buf = 0;
-  for (int step = 0; step + 1 < steps; ++step) {
-    // step + 1 lies in LDS, and so do the weights of this step; the buffer of step - 1 is free
-    if (kBufs > 3 && step + kBufs - 2 < steps) loads_done<(kBufs - 3) * kLoads>();  // later steps' loads go on
-    else loads_done();
+  // Waits until step + 1 lies in LDS, and the weights of this step; the buffer of step - 1 is free.  Loads go
+  // on past the last step, of its last key's record, so that as many are always under way.
+  auto turn = [&](int step) BSR_INLINE {
+    loads_done<(kBufs - 3) * kLoads>();
     barrier();
-    const int buf1 = buf + 1 == kBufs ? 0 : buf + 1, last = buf == 0 ? kBufs - 1 : buf - 1;
-    if (step % kIdSteps == 0 && step && step + kIdSteps < steps) load_ids(step + kIdSteps);
-    const bool more = step + kBufs - 1 < steps;
-    const int ahead = step + kBufs;  // its ids are read whether there is such a step or not (keys end at the last)
-    if (scores) {
+    if (step % kIdSteps == 0 && step) load_ids(step + kIdSteps);
+    rescale(step);
+  };
+  int buf = 0;
+  if (scores) {
+    for (int step = 0; step + 1 < steps; ++step) {
+      turn(step);
+      const int buf1 = buf + 1 == kBufs ? 0 : buf + 1, last = buf == 0 ? kBufs - 1 : buf - 1;
       f32x16 s[1];
       float unit;
+      start_values(step, buf);
       score(buf1, s[0], [&](int n) BSR_INLINE {
-        if (n < kLoads && more) load_unit(n, last);
-        if (n == 16) read_id(ahead);
-        if (n == 24) find_offset(ahead);
+        if (n < kValueProducts) value_product(step, buf, n);
+        if (n < kLoads) load_unit(n, last);
+        if (n == 16) read_id(step + kBufs);
+        if (n == 24) find_offset(step + kBufs);
       });
       settle(step + 1, s, &unit);
       leave_weights(step + 1, s[0], unit);
-    } else {
-      if (more) load_step(last);
-      read_id(ahead);
-      find_offset(ahead);
+      buf = buf1;
     }
-    rescale(step);
-    values(step, buf);
-    buf = buf1;
+  } else {  // (in a loop of its own: two ways round the value products would have the sums copied)
+    for (int step = 0; step + 1 < steps; ++step) {
+      turn(step);
+      load_step(buf == 0 ? kBufs - 1 : buf - 1);
+      read_id(step + kBufs);
+      values(step, buf);
+      find_offset(step + kBufs);
+      buf = buf + 1 == kBufs ? 0 : buf + 1;
+    }
   }
   if (steps > 0) {
+    loads_done();  // none may reach LDS that is no longer the workgroup's
     barrier();
     rescale(steps - 1);
     values(steps - 1, buf);
@@ -1148,9 +1214,9 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
 // joined them, always in the order of the parts.
 // ---------------------------------------------------------------------------
 constexpr int kJoinThreads = 128;
-// Parts of a range, at most: a part is at least 1.1 / target of the whole batch's keys.
-constexpr uint32_t kJoinParts = 512;
-static_assert(kMaxTarget / 1.1 + 2 < kJoinParts, "a range's parts fit");
+// Parts of a range, at most: of `target` for up to as many ranges, or of twice
+// that for more than `target` ranges, every other of which has a part too.
+constexpr uint32_t kJoinParts = kMaxTarget;
 
 // A workgroup joins rows that its threads hold four dimensions each of: one of
 // 512, or several of fewer.  The first sums are read beside the maxima, the others eight at a time.
@@ -1219,7 +1285,7 @@ hipError_t launch_join(const AttnParams& p, uint32_t base, hipStream_t s) {
 template <typename T, int kMods>
 hipError_t launch_tiles(const AttnParams& p, hipStream_t s) {
   const AttnTiling t = attn_tiling(p.n_requests, p.n_tokens, p.n_heads, p.n_kv_heads, p.v_dim, p.max_len);
-  const dim3 grid(static_cast<uint32_t>(t.base + p.target)), block(kAttnThreads);
+  const dim3 grid(static_cast<uint32_t>(t.items)), block(kAttnThreads);
   if (p.k_dim == 64) hipLaunchKernelGGL((k_attend_heads<T, 64, kMods>), grid, block, 0, s, p);
   else if (p.k_dim == 128) hipLaunchKernelGGL((k_attend_heads<T, 128, kMods>), grid, block, 0, s, p);
   else if (p.tile_rows == 32) hipLaunchKernelGGL((k_attend_latent<T, kMods, 1>), grid, block, 0, s, p);
@@ -1254,12 +1320,14 @@ AttnTiling attn_tiling(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
   t.units = n_kv_heads * ((per_kv + t.tile_heads - 1) / t.tile_heads);
   // every request may end a tile early; none has a tile without a token
   const uint64_t tiles = (n_tokens / t.tile_tokens) + static_cast<uint64_t>(n_requests < n_tokens ? n_requests : n_tokens);
-  t.base = tiles * t.units;
+  t.base = t.items = tiles * t.units;
   t.min_part = v_dim == 512 ? 64 : 128;
   if (max_len > t.min_part) {
-    t.target = v_dim == 512 ? 256 : kMaxTarget;  // workgroups that the GPU holds at once
+    t.target = v_dim == 512 ? 256 : v_dim == 128 ? 512 : kMaxTarget;  // workgroups that the GPU holds at once
+    const uint64_t parts = t.base <= t.target ? t.target : 2 * t.target;
     const uint64_t most = t.base * ((max_len + t.min_part - 1) / t.min_part);
-    t.slots = most < 2ull * t.target ? most : 2ull * t.target;
+    t.slots = most < parts ? most : parts;
+    if (t.items < t.slots) t.items = t.slots;
     t.workspace = t.slots * t.tile_rows * (v_dim + 2) * sizeof(float);
   }
   return t;

@@ -149,7 +149,7 @@ int attend(const bsr_ctx* c, const bsr_attn_args* a, bsr::AttnParams* p, void* s
   if (t.workspace && (!a->workspace || !aligned(a->workspace, 16) || a->workspace_bytes < t.workspace))
     return refuse(BSR_E_ARG, "workspace is NULL, not 16-byte aligned or smaller than %llu bytes",
                   static_cast<unsigned long long>(t.workspace));
-  if (t.base + t.target >= (1ull << 24)) return refuse(BSR_E_ARG, "too many rows and heads for one launch");
+  if (t.items >= (1ull << 24)) return refuse(BSR_E_ARG, "too many rows and heads for one launch");
   p->tile_rows = t.tile_rows;
   p->tile_heads = t.tile_heads;
   p->tile_tokens = t.tile_tokens;

@@ -95,11 +95,12 @@ struct AttnParams {
 
 // An attention tile is up to kTileRows query rows (tokens x heads of one KV head).
 constexpr uint32_t kTileRows = 128;
-constexpr uint32_t kMaxTarget = 512;
+constexpr uint32_t kMaxTarget = 768;
 
 struct AttnTiling {
   uint32_t tile_rows, tile_heads, tile_tokens, units, target, min_part;
   uint64_t base;      // tiles x units of the batch, at most
+  uint64_t items;     // parts of them, at most
   uint64_t slots;     // partial results, at most
   uint64_t workspace; // bytes
 };
