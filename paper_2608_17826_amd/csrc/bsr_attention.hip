@@ -81,7 +81,7 @@ __device__ __forceinline__ int64_t record_at(const AttnParams& p, const Request&
   const uint32_t b = p.div_block.div(j);
   const int32_t id = q.table[b];
   if (id < 0 || static_cast<uint32_t>(id) >= p.pool_blocks) return -1;
-  return static_cast<int64_t>(id) * p.block_bytes + static_cast<int64_t>(j - b * p.div_block.d) * p.record_bytes;
+  return static_cast<int64_t>(static_cast<uint64_t>(id) * p.block_bytes + (j - b * p.div_block.d) * p.record_bytes);
 }
 
 // One row over the keys [lo, hi) by one wave: 64 keys at a time, a lane each
@@ -337,7 +337,7 @@ __device__ __forceinline__ void mfma_next(f32x16& c, s16x8 a, s16x8 b) {
   if (__is_same(T, __bf16)) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
   else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
 }
-__device__ __forceinline__ void mfma_done(f32x16& c) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(c)); }
+__device__ __forceinline__ void mfma_done(f32x16& c, f32x16& d) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(c), "+v"(d)); }
 
 template <typename T>
 __device__ __forceinline__ s16x8 to_half(const float* x) {
@@ -375,10 +375,18 @@ __device__ __forceinline__ uint32_t lds_at(const void* p) {
 __device__ __forceinline__ void load_to_lds(const uint8_t* src, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory");
 }
-// The same from a scalar address and a lane's offset (a vector instruction
-// that wrote the address, unseen by the compiler to be followed by a load, is five wait states back).
-__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+// The same from a scalar address plus a lane's offset.  (A load must not follow
+// closely on a vector instruction that wrote its scalar address, and the compiler sees no load here: the
+// address comes from two scalar additions.)
+__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t lo, uint32_t hi, uint32_t offset, uint32_t lds) {
+  const uint64_t b = reinterpret_cast<uint64_t>(base);
+  uint32_t x, y;
+  asm volatile("s_add_u32 %0, %2, %4\n\ts_addc_u32 %1, %3, %5"
+               : "=&s"(x), "=s"(y)
+               : "s"(static_cast<uint32_t>(b)), "s"(static_cast<uint32_t>(b >> 32)), "s"(lo), "s"(hi)
+               : "scc");
+  const uint64_t at = static_cast<uint64_t>(y) << 32 | x;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(at) : "memory");
 }
 // 64 lanes x 4 bytes likewise.
 __device__ __forceinline__ void load_words_to_lds(const void* src, uint32_t lds) {
@@ -642,7 +650,7 @@ __device__ __forceinline__ bool key_offset(const AttnParams& p, const KeyLoad& k
   const bool ok = static_cast<uint32_t>(k.id) < p.pool_blocks;  // (fewer than 2^31)
   const uint32_t keep = 0u - static_cast<uint32_t>(ok);  // no branch: latent steps do this beside their products
   const uint32_t id = k.id & keep, at = (k.j - k.block * p.div_block.d) & keep;
-  *off = static_cast<int64_t>(id) * p.block_bytes + at * p.record_bytes;  // a block is smaller than 2^31 bytes
+  *off = static_cast<int64_t>(static_cast<uint64_t>(id) * p.block_bytes + at * p.record_bytes);  // a block is smaller than 2^31 bytes
   return ok;
 }
 
@@ -894,9 +902,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   constexpr int kKeys = kStep / 4, kIdSteps = 64 / kKeys;  // keys that a wave loads at a step; steps of one load of block ids
   constexpr int kN = KD / 16, kAhead = 3;
   constexpr int kHeld = kBlocks == 4 ? 32 : kN;  // products whose queries lie in registers; the others' are read from LDS
-  // A product that goes on with the last one's sum waits for it, twice as long as it takes itself: scores
-  // alternate between two sums, or, where registers are short, with the value products.
-  constexpr int kSums = kBlocks == 4 ? 1 : 2;
+  // Two sums in turn: a product that goes on with the last one's sum waits for it, twice as long as it takes itself.
+  constexpr int kSums = 2;
   __shared__ __attribute__((aligned(1024))) uint8_t tiles[kBufs][kTileBytes];
   __shared__ __attribute__((aligned(16))) uint8_t weights[2][kBlocks][2][1024];  // [step][rows / 32][16 keys][lane]
   __shared__ float backs[2][32 * kBlocks];
@@ -957,19 +964,19 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     const int j = key_at(first_step + lane / kKeys, lane % kKeys);
     load_words_to_lds(q.table + p.div_block.div(j), lds_at(&block_ids[wave][first_step / kIdSteps & 1][0]));
   };
-  // the offset of the lane's record, key lane % 8 of a step: its block id is read some time before
-  int32_t id = 0;
+  // The offset of the lane's record, key lane % 8 of a step, in strides (the block id is read from
+  // LDS, the others are a few instructions each).
+  KeyLoad key{};
   int64_t offset = 0;
-  auto read_id = [&](int step) BSR_INLINE {
-    id = block_ids[wave][step / kIdSteps & 1][step % kIdSteps * kKeys + lane % kKeys];
-  };
-  auto find_offset = [&](int step) BSR_INLINE {
-    const int j = key_at(step, lane % kKeys);
-    const KeyLoad k{j, p.div_block.div(j), id};
-    const bool ok = key_offset(p, k, &offset);
-    const uint64_t bad = ~__ballot(ok);
-    // (by every lane: what stands beside the products stays one block of instructions)
-    outside[step & 7][wave] = static_cast<uint8_t>(bad);
+  auto find_offset = [&](int step, int stride) BSR_INLINE {
+    if (stride == 0) key.id = block_ids[wave][step / kIdSteps & 1][step % kIdSteps * kKeys + lane % kKeys];
+    if (stride == 1) key.j = key_at(step, lane % kKeys);
+    if (stride == 2) key.block = p.div_block.div(key.j);
+    if (stride == 3) {
+      const bool ok = key_offset(p, key, &offset);
+      // by every lane: what stands beside the products stays one block of instructions
+      outside[step & 7][wave] = static_cast<uint8_t>(~__ballot(ok));
+    }
   };
   // load n of a step: the values of record n, or the rest of all; units of 16
   // bytes are permuted by the record's row
@@ -977,9 +984,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     const uint32_t to = tiles_at + buf * kTileBytes + wave * kWaveBytes + n * 1024;
     const uint32_t lo = static_cast<uint32_t>(offset), hi = static_cast<uint32_t>(offset >> 32);
     if (n < kKeys) {
-      const uint64_t off = static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(hi, n))) << 32 |
-                           static_cast<uint32_t>(__builtin_amdgcn_readlane(lo, n));
-      load_to_lds(p.k_pool + off, (lane ^ unit_swap<128>(wave * kKeys + n)) * 16, to);
+      load_to_lds(p.k_pool, __builtin_amdgcn_readlane(lo, n), __builtin_amdgcn_readlane(hi, n),
+                  (lane ^ unit_swap<128>(wave * kKeys + n)) * 16, to);
     } else {
       const int r = lane >> 3;
       const uint64_t off = static_cast<uint64_t>(__shfl(hi, r)) << 32 | __shfl(lo, r);
@@ -1002,10 +1008,9 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   for (int e = 0; e < 2; ++e)
     v_at[e] = e * kWaveBytes + v_row * kValueBytes + wave * 256 + ((v_unit ^ unit_swap<128>(v_row + 8 * e)) * 16) + (lane & 1) * 8;
 
-  // Products of the wave's rows with the 32 keys in buffer `buf`; `beside(n)` goes on
-  // beside them, the value products of another step among it.  Reads of LDS run kAhead
-  // products ahead; the order is pinned.
-  auto score = [&](int buf, f32x16& s, auto beside) BSR_INLINE {
+  // Products of the wave's rows with the 32 keys in buffer `buf`.  Reads of LDS run kAhead products
+  // ahead; beside(n) goes on beside them, after() while the last ones end; the order is pinned.
+  auto score = [&](int buf, f32x16& s, auto beside, auto after) BSR_INLINE {
     const uint32_t at = tiles_at + buf * kTileBytes;
     auto k_row = [&](int n) BSR_INLINE {
       return n < VD / 16 ? lds_row16(at + (k_at ^ (n % 8 * 32)) + n / 8 * 256) : lds_row16(at + (k_rest ^ ((n - VD / 16) * 32)));
@@ -1024,12 +1029,10 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
       beside(n);
       __builtin_amdgcn_sched_barrier(0);
     }
-    mfma_done(sums[0]);
-    s = sums[0];
-    if (kSums == 2) {
-      mfma_done(sums[kSums - 1]);
-      s += sums[kSums - 1];
-    }
+    after();
+    __builtin_amdgcn_sched_barrier(0);
+    mfma_done(sums[0], sums[1]);
+    s = sums[0] + sums[1];
   };
   // their scores, what the rows see of them, and the running maximum
   auto settle = [&](int step, f32x16 (&s)[1], float* unit) BSR_INLINE {
@@ -1053,14 +1056,17 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     if (rise && half == 0) backs[step & 1][row] = back;
     if (lane == 0) rises[step & 1][wave] = rise;
   };
-  auto leave_weights = [&](int step, f32x16& s, float unit) BSR_INLINE {
-    l += weigh(s, unit, m > -__builtin_inff() ? m : 0.0f);
+  // scores [from, to) to weights; each eight of them then go to LDS
+  auto leave_weights = [&](int step, f32x16& s, float unit, float base, int from, int to) BSR_INLINE {
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int e = from; e < to; ++e) {
+      s[e] = exp2_(__builtin_fmaf(s[e], unit, -base));
+      l += s[e];
+      if (e % 8 != 7) continue;
       float x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = s[8 * n + e];
-      *(BSR_LDS s16x8*)(uintptr_t)(weights_at + (((step & 1) * kBlocks + wave) * 2 + n) * 1024 + lane * 16) = to_half<T>(x);
+      for (int i = 0; i < 8; ++i) x[i] = s[e - 7 + i];
+      *(BSR_LDS s16x8*)(uintptr_t)(weights_at + (((step & 1) * kBlocks + wave) * 2 + e / 8) * 1024 + lane * 16) = to_half<T>(x);
     }
   };
   auto rescale = [&](int step) BSR_INLINE {
@@ -1110,8 +1116,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     load_ids(kIdSteps);
 #pragma unroll
     for (int i = 0; i < kBufs; ++i) {
-      read_id(i);
-      find_offset(i);
+      for (int stride = 0; stride < 4; ++stride) find_offset(i, stride);
       if (i < kBufs - 1) load_step(i);
     }
     loads_done<(kBufs - 2) * kLoads>();
@@ -1119,9 +1124,9 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     if (scores) {
       f32x16 s[1];
       float unit;
-      score(0, s[0], [](int) {});
+      score(0, s[0], [](int) {}, [] {});
       settle(0, s, &unit);
-      leave_weights(0, s[0], unit);
+      leave_weights(0, s[0], unit, m > -__builtin_inff() ? m : 0.0f, 0, 16);
     }
   }
   // Waits until step + 1 lies in LDS, and the weights of this step; the buffer of step - 1 is free.  Loads go
@@ -1139,24 +1144,33 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
       const int buf1 = buf + 1 == kBufs ? 0 : buf + 1, last = buf == 0 ? kBufs - 1 : buf - 1;
       f32x16 s[1];
       float unit;
-      start_values(step, buf);
+      // the scores of step + 1, with the next loads beside them; then the values of this step, with the softmax of the next
+      // beside them
       score(buf1, s[0], [&](int n) BSR_INLINE {
-        if (n < kValueProducts) value_product(step, buf, n);
         if (n < kLoads) load_unit(n, last);
-        if (n == 16) read_id(step + kBufs);
-        if (n == 24) find_offset(step + kBufs);
+        if (n >= 12 && n < 28 && n % 4 == 0) find_offset(step + kBufs, (n - 12) / 4);
+        if (n == kN - 3) start_values(step, buf);
+      }, [&]() BSR_INLINE {
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) value_product(step, buf, i);
       });
       settle(step + 1, s, &unit);
-      leave_weights(step + 1, s[0], unit);
+      const float base = m > -__builtin_inff() ? m : 0.0f;
+      constexpr int kRest = kValueProducts - kBlocks;
+#pragma unroll
+      for (int i = 0; i < kRest; ++i) {
+        value_product(step, buf, kBlocks + i);
+        leave_weights(step + 1, s[0], unit, base, i * 16 / kRest, (i + 1) * 16 / kRest);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       buf = buf1;
     }
   } else {  // (in a loop of its own: two ways round the value products would have the sums copied)
     for (int step = 0; step + 1 < steps; ++step) {
       turn(step);
       load_step(buf == 0 ? kBufs - 1 : buf - 1);
-      read_id(step + kBufs);
       values(step, buf);
-      find_offset(step + kBufs);
+      for (int stride = 0; stride < 4; ++stride) find_offset(step + kBufs, stride);
       buf = buf + 1 == kBufs ? 0 : buf + 1;
     }
   }
