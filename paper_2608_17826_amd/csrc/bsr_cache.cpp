@@ -234,7 +234,7 @@ int bsr_cache_append(bsr_ctx* c, const bsr_append_args* a, void* stream) {
   bsr::AppendParams p{};
   p.slots = a->slots;
   p.pool = static_cast<uint8_t*>(a->pool);
-  p.vector = d.record_bytes % 16 == 0;
+  p.vector = planar || d.record_bytes % 16 == 0;
   for (uint32_t i = 0; i < a->n_sources; ++i) {
     p.src[i] = static_cast<const uint8_t*>(a->src[i]);
     p.src_stride[i] = a->src_stride[i] * size;
@@ -250,6 +250,7 @@ int bsr_cache_append(bsr_ctx* c, const bsr_append_args* a, void* stream) {
   p.n_slots = static_cast<uint64_t>(a->pool_blocks) * d.block_tokens;
   p.units = static_cast<uint32_t>(p.vector ? values / 8 : values);
   p.div_units = bsr::make_fastdiv(p.units);
+  p.div_block = bsr::make_fastdiv(d.block_tokens);
   if (!planar && static_cast<uint64_t>(a->n_tokens) * p.units >= (1ull << 32) - 256)
     return refuse(BSR_E_ARG, "too many values for one launch");
   return enqueue(c, "bsr_cache_append", [&] { return bsr::launch_append(p, static_cast<hipStream_t>(stream)); });

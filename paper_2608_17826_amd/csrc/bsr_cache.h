@@ -54,7 +54,8 @@ struct AppendParams {
   uint64_t n_slots;       // pool_blocks * block_tokens
   FastDiv div_units;      // CONTIG: by the units of a record
   uint32_t units;         // CONTIG: 8-value units of a record, or its values
-  uint32_t vector;        // CONTIG: whole units of 8 values, 16-byte aligned everywhere
+  uint32_t vector;        // whole units of 8 values, 16-byte aligned everywhere (PLANAR: in the source)
+  FastDiv div_block;      // by block_tokens
 };
 hipError_t launch_append(const AppendParams& p, hipStream_t s);
 
