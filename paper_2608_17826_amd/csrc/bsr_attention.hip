@@ -212,11 +212,12 @@ __device__ __forceinline__ uint32_t wave_sum(const AttnParams& p, uint32_t x) { 
 
 // Keys of a part.  Where the batch has no more tiles x units than the GPU holds
 // workgroups (target), its ranges are cut into as many parts as those, so that all run at
-// once and end together; up to twice as many tiles are cut into twice as many parts; more are
-// left whole.  All parts have the same length, which starts at their share
+// once and end together; up to twice as many tiles are cut into twice as many
+// parts if those are long (kLongPart) and no documents make the ranges uncertain; more are left whole.  All parts have the same length, which starts at their share
 // of the batch's (tile, key) pairs and grows until the parts, each range's
 // rounded up, are no more than that.  Past six rounds, and for batches of over 64 requests,
 // it is the length that no rounding makes too many of.
+constexpr float kLongPart = 2048;  // keys
 __device__ __forceinline__ uint32_t part_keys(const AttnParams& p, const RequestWork& first) {
   constexpr uint32_t kWhole = 0x7fffffffu;
   if (!p.target) return kWhole;
@@ -237,8 +238,8 @@ __device__ __forceinline__ uint32_t part_keys(const AttnParams& p, const Request
     total = wave_total(total);
   }
   const uint32_t limit = base <= p.target ? p.target : 2 * p.target;
-  if (base >= limit) return kWhole;
   total *= static_cast<float>(p.units);
+  if (base >= limit || (base > p.target && (p.documents || total < kLongPart * static_cast<float>(limit)))) return kWhole;
   const auto length = [&](float keys) {  // whole steps; the sum is off by less than a thousandth (2^14 additions a lane)
     const uint32_t k = static_cast<uint32_t>(fminf(keys * 1.002f, 2e9f)) + 1;
     return uniform(((k > p.min_part ? k : p.min_part) + 63) & ~63u);
@@ -512,12 +513,13 @@ __device__ __forceinline__ ScoreMods score_mods(const AttnParams& p) {
 
 template <int kMods>
 __device__ __forceinline__ void modify(const ScoreMods& m, float slope2, int pos, int j0, f32x16& s) {
+  const float away = static_cast<float>(pos - j0);
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
     float x = s[e];
     if (kMods & kCap) x = m.cap2 - 2 * m.cap2 * __builtin_amdgcn_rcpf(exp2_(x * m.in_cap) + 1);
     else x *= m.unit;
-    if (kMods & kSlopes) x = __builtin_fmaf(-slope2, fabsf(static_cast<float>(pos - (j0 + 8 * (e / 4) + e % 4))), x);
+    if (kMods & kSlopes) x = __builtin_fmaf(-slope2, fabsf(away - static_cast<float>(8 * (e / 4) + e % 4)), x);
     s[e] = x;
   }
 }
@@ -709,13 +711,6 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
   cut(w, lo, hi, &k0, &k1);
   const int steps = (k1 - k0 + kStep - 1) / kStep;
 
-  s16x8 qf[D / 16];
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    qf[s] = s16x8{};
-    if (t.real)
-      qf[s] = *reinterpret_cast<const s16x8*>(p.q + (q.first + t.i) * p.q_token + t.head * p.q_head + s * 32 + half * 16);
-  }
   f32x16 o[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
@@ -737,7 +732,19 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
       load_to_lds(v_base + off, to + kTileBytes);
     }
   };
-  KeyLoad next{};
+  KeyLoad next{}, k_first{}, k_second{};
+  if (wave == 0 && steps > 0) {  // (steps past the last read its last key's block id)
+    k_first = key_load(p, q, k0 + lane, k1 - 1);
+    k_second = key_load(p, q, k0 + kStep + lane, k1 - 1);
+    next = key_load(p, q, k0 + 2 * kStep + lane, k1 - 1);
+  }
+  s16x8 qf[D / 16];
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    qf[s] = s16x8{};
+    if (t.real)
+      qf[s] = *reinterpret_cast<const s16x8*>(p.q + (q.first + t.i) * p.q_token + t.head * p.q_head + s * 32 + half * 16);
+  }
   auto put_offsets = [&](int step, const KeyLoad& k) BSR_INLINE {  // by wave 0
     int64_t off;
     const bool ok = key_offset(p, k, &off);
@@ -746,9 +753,7 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
     if (lane == 0) outside[step & 3] = bad;
   };
   if (steps > 0) {
-    if (wave == 0) {  // (steps past the last read its last key's block id)
-      const KeyLoad k_first = key_load(p, q, k0 + lane, k1 - 1), k_second = key_load(p, q, k0 + kStep + lane, k1 - 1);
-      next = key_load(p, q, k0 + 2 * kStep + lane, k1 - 1);
+    if (wave == 0) {
       put_offsets(0, k_first);
       put_offsets(1, k_second);
     }
@@ -941,13 +946,6 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   const int steps = (k1 - k0 + kStep - 1) / kStep;
 
   s16x8 qf[kHeld];
-#pragma unroll
-  for (int n = 0; n < kN; ++n) {
-    s16x8 x{};
-    if (t.real) x = *reinterpret_cast<const s16x8*>(p.q + (q.first + t.i) * p.q_token + t.head * p.q_head + n * 32 + half * 16);
-    if (n < kHeld) qf[n] = x;
-    else *reinterpret_cast<s16x8*>(&queries[wave][n - kHeld][lane * 16]) = x;
-  }
   f32x16 o[kBlocks][4];
 #pragma unroll
   for (int b = 0; b < kBlocks; ++b)
@@ -1112,8 +1110,17 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
 
   if (steps > 0) {
     load_ids(0);
-    loads_done();
     load_ids(kIdSteps);
+  }
+#pragma unroll
+  for (int n = 0; n < kN; ++n) {
+    s16x8 x{};
+    if (t.real) x = *reinterpret_cast<const s16x8*>(p.q + (q.first + t.i) * p.q_token + t.head * p.q_head + n * 32 + half * 16);
+    if (n < kHeld) qf[n] = x;
+    else *reinterpret_cast<s16x8*>(&queries[wave][n - kHeld][lane * 16]) = x;
+  }
+  if (steps > 0) {
+    loads_done();
 #pragma unroll
     for (int i = 0; i < kBufs; ++i) {
       for (int stride = 0; stride < 4; ++stride) find_offset(i, stride);
@@ -1227,73 +1234,109 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
 // Joins the parts of a row: sums and maxima as the running softmax would have
 // joined them, always in the order of the parts.
 // ---------------------------------------------------------------------------
-constexpr int kJoinThreads = 128;
 // Parts of a range, at most: of `target` for up to as many ranges, or of twice
 // that for more than `target` ranges, every other of which has a part too.
 constexpr uint32_t kJoinParts = kMaxTarget;
+constexpr uint32_t kJoinRun = 8;  // parts that a thread sums, about
 
-// A workgroup joins rows that its threads hold four dimensions each of: one of
-// 512, or several of fewer.  The first sums are read beside the maxima, the others eight at a time.
-template <typename T, int VD>
+__host__ __device__ __forceinline__ uint32_t teams_of(uint64_t parts, uint32_t most) {
+  uint32_t teams = 1;
+  while (teams < most && teams * kJoinRun < parts) teams *= 2;
+  return teams;
+}
+
+// A team of kSlice / 4 threads holds four dimensions each of a row (of kSlice of them) and sums every
+// teams-th part; the teams of a row meet in LDS.  One row takes all teams from 8 parts a
+// team on; fewer parts leave room for several rows.  A team's first sums are read beside the maxima.
+template <typename T, int VD, int kSlice, uint32_t kJoinThreads>
 __global__ __launch_bounds__(kJoinThreads) void k_attend_join(AttnParams p, uint32_t rows_per) {
-  constexpr uint32_t kVecs = VD / 4, kSide = kJoinThreads / kVecs;  // threads of a row; rows side by side
-  constexpr uint32_t kFirst = 8;
-  __shared__ float part_m[kSide][kJoinParts], part_l[kSide][kJoinParts];
+  constexpr uint32_t kVecs = kSlice / 4, kTeams = kJoinThreads / kVecs;
+  constexpr uint32_t kStats = kJoinParts > kTeams * kJoinRun ? kJoinParts : kTeams * kJoinRun;  // of all rows at once
+  __shared__ __attribute__((aligned(16))) float part_m[kStats], part_l[kStats];
+  __shared__ f32x4 sums[kJoinThreads];
+  __shared__ float sums_l[kTeams];
   Work w;
   Request q;
   if (!find_work<true>(p, blockIdx.x, &w, &q) || w.n_splits < 2) return;
-  const uint32_t side = threadIdx.x / kVecs, at = threadIdx.x % kVecs, n = w.n_splits;
+  const uint32_t n = w.n_splits, team = threadIdx.x / kVecs, at = threadIdx.x % kVecs, d = (blockIdx.z * kVecs + at) * 4;
+  const uint32_t teams = teams_of(n, kTeams);  // of a row
+  const uint32_t side = kTeams / teams, mine = team / teams, first = team % teams;
   const uint64_t step = static_cast<uint64_t>(p.tile_rows) * VD;
-  for (uint32_t r0 = blockIdx.y * rows_per; r0 < (blockIdx.y + 1) * rows_per; r0 += kSide) {
-    const uint32_t row = r0 + side;
-    const TileRows t = tile_row(p, q, w, row);
+  const uint32_t n4 = (n + 3) & ~3u, stats = mine * n4;  // (at most kJoinRun parts a row where several rows are side by side)
+  for (uint32_t r0 = blockIdx.y * rows_per; r0 < (blockIdx.y + 1) * rows_per; r0 += side) {
+    const uint32_t row = r0 + mine;
+    TileRows t = tile_row(p, q, w, row);
+    t.real = t.real && row < (blockIdx.y + 1) * rows_per;
     const float* ml = p.part_ml + (static_cast<uint64_t>(w.slot) * p.tile_rows + row) * 2;
-    const float* part = p.part + (static_cast<uint64_t>(w.slot) * p.tile_rows + row) * VD + at * 4;
-    f32x4 first[kFirst];
+    const float* part = p.part + (static_cast<uint64_t>(w.slot) * p.tile_rows + row) * VD + d;
+    f32x4 ahead[kJoinRun];
     if (t.real) {
 #pragma unroll
-      for (uint32_t s = 0; s < kFirst; ++s) first[s] = *reinterpret_cast<const f32x4*>(part + min(s, n - 1) * step);
-      for (uint32_t s = at; s < n; s += kVecs) {
-        part_m[side][s] = ml[static_cast<uint64_t>(s) * p.tile_rows * 2];
-        part_l[side][s] = ml[static_cast<uint64_t>(s) * p.tile_rows * 2 + 1];
+      for (uint32_t i = 0; i < kJoinRun; ++i)
+        ahead[i] = *reinterpret_cast<const f32x4*>(part + min(first + i * teams, n - 1) * step);
+      for (uint32_t s = first * kVecs + at; s < n4; s += teams * kVecs) {
+        part_m[stats + s] = s < n ? ml[static_cast<uint64_t>(s) * p.tile_rows * 2] : -__builtin_inff();
+        part_l[stats + s] = s < n ? ml[static_cast<uint64_t>(s) * p.tile_rows * 2 + 1] : 0.0f;
       }
     }
     __syncthreads();
     float m = -__builtin_inff(), l = 0;
     f32x4 x{};
     if (t.real) {
-#pragma unroll 8
-      for (uint32_t s = 0; s < n; ++s) m = fmaxf(m, part_m[side][s]);
+#pragma unroll 4
+      for (uint32_t s = 0; s < n4; s += 4) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(&part_m[stats + s]);
+        m = fmaxf(fmaxf(fmaxf(m, v[0]), fmaxf(v[1], v[2])), v[3]);
+      }
       const float from = m > -__builtin_inff() ? m : 0.0f;
-      const auto add = [&](uint32_t s, f32x4 sums) BSR_INLINE {
-        const float ls = part_l[side][s];
-        // a part without a seen key weighs nothing
-        const float f = ls == 0 ? 0.0f : exp2_(part_m[side][s] - from);
+      const auto add = [&](uint32_t s, f32x4 part_sums) BSR_INLINE {
+        const float ls = part_l[stats + s];
+        const float f = ls == 0 ? 0.0f : exp2_(part_m[stats + s] - from);  // a part without a seen key weighs nothing
         l += f * ls;
-        x += f * sums;
+        x += f * part_sums;
       };
 #pragma unroll
-      for (uint32_t s = 0; s < kFirst; ++s)
-        if (s < n) add(s, first[s]);
-#pragma unroll 8
-      for (uint32_t s = kFirst; s < n; ++s) add(s, *reinterpret_cast<const f32x4*>(part + s * step));
+      for (uint32_t i = 0; i < kJoinRun; ++i)
+        if (first + i * teams < n) add(first + i * teams, ahead[i]);
+#pragma unroll 4
+      for (uint32_t s = first + kJoinRun * teams; s < n; s += teams) add(s, *reinterpret_cast<const f32x4*>(part + s * step));
+    }
+    sums[threadIdx.x] = x;
+    if (at == 0) sums_l[team] = l;
+    __syncthreads();
+    if (t.real && first == 0) {
+      for (uint32_t i = 1; i < teams; ++i) {
+        x += sums[threadIdx.x + i * kVecs];
+        l += sums_l[team + i];
+      }
       const Sink sink{false, 0};
       x *= l == 0 ? 0.0f : 1.0f / l;
-      put4<T>(p, q, t, sink, row, at * 4, x);
-      if (at == 0) put_stats(p, q, t, sink, row, m, l);
+      put4<T>(p, q, t, sink, row, d, x);
+      if (d == 0) put_stats(p, q, t, sink, row, m, l);
     }
     __syncthreads();
   }
 }
 
-template <typename T, int VD>
-hipError_t launch_join(const AttnParams& p, uint32_t base, hipStream_t s) {
-  const uint32_t rows = p.tile_tokens * p.tile_heads, side = kJoinThreads / (VD / 4);
-  // rows of a workgroup: one pass of its threads where tiles are few, more where their number alone fills the GPU
-  uint32_t per = side;
-  while (per < rows && static_cast<uint64_t>(base) * ((rows + per - 1) / per) > 8192) per *= 2;
-  hipLaunchKernelGGL((k_attend_join<T, VD>), dim3(base, (rows + per - 1) / per), dim3(kJoinThreads), 0, s, p, per);
+template <typename T, int VD, int kSlice, uint32_t kThreads>
+hipError_t launch_join(const AttnParams& p, const AttnTiling& t, hipStream_t s) {
+  const uint32_t rows = p.tile_tokens * p.tile_heads, teams = kThreads / (kSlice / 4);
+  // rows of a workgroup: as many as its teams take at once if the parts spread evenly over the tiles there may
+  // be, more where the tiles alone fill the GPU
+  uint32_t per = teams / teams_of(t.slots / t.base, teams);
+  while (per < rows && t.base * ((rows + per - 1) / per) > 8192) per *= 2;
+  hipLaunchKernelGGL((k_attend_join<T, VD, kSlice, kThreads>), dim3(static_cast<uint32_t>(t.base), (rows + per - 1) / per, VD / kSlice),
+                     dim3(kThreads), 0, s, p, per);
   return hipGetLastError();
+}
+
+// Few tiles, each in many parts: 16 teams for 128 dimensions of a row.  One
+// latent token over 128K (16 rows, 256 parts): 21.2 us with the teams of the others, 9.3 so; 22 latent tiles in 256 parts:
+// 13.2 and 17.8.
+template <typename T, int VD>
+hipError_t launch_join(const AttnParams& p, const AttnTiling& t, hipStream_t s) {
+  if (t.base <= 4) return launch_join<T, VD, (VD < 128 ? VD : 128), 512>(p, t, s);
+  return launch_join<T, VD, VD, 128>(p, t, s);
 }
 
 template <typename T, int kMods>
@@ -1307,8 +1350,7 @@ hipError_t launch_tiles(const AttnParams& p, hipStream_t s) {
   else hipLaunchKernelGGL((k_attend_latent<T, kMods, 4>), grid, block, 0, s, p);
   if (hipError_t e = hipGetLastError()) return e;
   if (!p.target) return hipSuccess;
-  const uint32_t base = static_cast<uint32_t>(t.base);
-  return p.v_dim == 64 ? launch_join<T, 64>(p, base, s) : p.v_dim == 128 ? launch_join<T, 128>(p, base, s) : launch_join<T, 512>(p, base, s);
+  return p.v_dim == 64 ? launch_join<T, 64>(p, t, s) : p.v_dim == 128 ? launch_join<T, 128>(p, t, s) : launch_join<T, 512>(p, t, s);
 }
 
 template <typename T>
