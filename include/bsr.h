@@ -660,8 +660,8 @@ int bsr_cache_append(bsr_ctx* ctx, const bsr_append_args* args, void* stream);
 typedef struct bsr_attn_args {
   uint32_t group;       /* of the context's layout: CONTIG, record_bytes a multiple of 16 */
   uint32_t dtype;       /* of q, out and the cache: BSR_TYPE_BF16 or F16 */
-  uint32_t n_requests;  /* 0 does nothing */
-  uint32_t n_tokens;    /* rows of q, out, lse; those at starts[n_requests] and after stay as they are */
+  uint32_t n_requests;  /* < 2^20; 0 does nothing */
+  uint32_t n_tokens;    /* < 2^24: rows of q, out, lse; those at starts[n_requests] and after stay as they are */
   uint32_t n_heads;     /* a multiple of n_kv_heads */
   uint32_t n_kv_heads;
   uint32_t k_dim, v_dim; /* (64, 64), (128, 128), or (576, 512): latent records, one KV head, whose value is
@@ -681,8 +681,8 @@ typedef struct bsr_attn_args {
   const int32_t* starts;       /* int32[n_requests + 1], not decreasing */
   const int32_t* lens;         /* int32[n_requests], at most max_len and what the table holds (taken as that
                                   where they are more) */
-  uint32_t max_len;            /* bound of lens that the host knows, < 2^31 */
-  uint32_t window;             /* 0, or how many keys up to its own position a row sees at most */
+  uint32_t max_len;            /* bound of lens that the host knows, < 2^30 */
+  uint32_t window;             /* < 2^30: 0, or how many keys up to its own position a row sees at most */
   float scale;                 /* > 0 */
   float softcap;               /* 0, or c > 0: the score is c * tanh(scale * q.k / c) */
   void* workspace;             /* bsr_attn_workspace_bytes, 16-byte aligned; contents need not be kept */

@@ -6,7 +6,7 @@
 // l: new keys scale what was summed so far by exp(m - m').
 #include <hip/hip_runtime.h>
 
-#include "bsr_cache.h"
+#include "bsr_attn_rows.h"
 
 namespace bsr {
 namespace {
@@ -16,72 +16,11 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// One request of the batch: its rows [first, first + rows) and its keys [0, n);
-// row i stands at base + i.
-struct Request {
-  int first, rows, n, base;
-  const int32_t* table;
-};
-
-__device__ __forceinline__ Request request_of(const AttnParams& p, uint32_t r) {
-  Request q;
-  const int cap = static_cast<int>(p.n_tokens);
-  q.first = min(max(p.starts[r], 0), cap);
-  q.rows = min(max(p.starts[r + 1], q.first), cap) - q.first;
-  q.n = min(max(p.lens[r], 0), static_cast<int>(p.max_len));
-  q.base = q.n - q.rows;
-  q.table = p.tables + static_cast<uint64_t>(r) * p.table_stride;
-  return q;
-}
-
-// What row i of a request sees: keys [lo, hi), those from base on by the bits
-// of its mask in a tree; and its position, from which distances count.
-struct Row {
-  int lo, hi, pos;
-  const uint64_t* mask;
-};
-
-__device__ __forceinline__ Row row_of(const AttnParams& p, const Request& q, uint32_t r, int i) {
-  Row w;
-  w.mask = nullptr;
-  if (p.tree) {
-    w.mask = p.tree + static_cast<uint64_t>(q.first + i) * p.tree_words;
-    int bits = 0;
-    if (p.window)
-      for (uint32_t k = 0; k < p.tree_words; ++k) bits += __popcll(w.mask[k]);
-    w.pos = q.base + bits - 1;
-    w.hi = q.n;
-  } else {
-    w.pos = q.base + i;
-    w.hi = w.pos + 1;
-    if (p.prefix) w.hi = max(w.hi, min(p.prefix[r], q.n));
-  }
-  w.lo = 0;
-  if (p.window) w.lo = max(0, w.pos - static_cast<int>(p.window) + 1);
-  if (p.documents) w.lo = max(w.lo, p.documents[q.first + i]);
-  return w;
-}
-
-__device__ __forceinline__ bool sees(const AttnParams& p, const Request& q, const Row& w, int j) {
-  if (j < w.lo || j >= w.hi) return false;
-  if (!w.mask || j < q.base) return true;
-  const uint32_t k = static_cast<uint32_t>(j - q.base);
-  return k < 64 * p.tree_words && (w.mask[k >> 6] >> (k & 63) & 1);
-}
-
 // Score times log2(e) of a product.
 __device__ __forceinline__ float score2(const AttnParams& p, float qk, float slope, int away) {
   float s = qk * p.scale;
   if (p.softcap > 0) s = p.softcap * tanhf(s / p.softcap);
   return (s - slope * static_cast<float>(abs(away))) * kLog2e;
-}
-
-// Byte offset of token j's record in a pool, or -1 where its block lies outside.
-__device__ __forceinline__ int64_t record_at(const AttnParams& p, const Request& q, int j) {
-  const uint32_t b = p.div_block.div(j);
-  const int32_t id = q.table[b];
-  if (id < 0 || static_cast<uint32_t>(id) >= p.pool_blocks) return -1;
-  return static_cast<int64_t>(static_cast<uint64_t>(id) * p.block_bytes + (j - b * p.div_block.d) * p.record_bytes);
 }
 
 // One row over the keys [lo, hi) by one wave: 64 keys at a time, a lane each
@@ -145,14 +84,6 @@ __device__ void attend_row(const AttnParams& p, const Request& q, const Row& w, 
 // kernel joins them.  Every workgroup finds its item from the lengths alone:
 // nothing about them is known to the host.
 // ---------------------------------------------------------------------------
-struct Work {
-  uint32_t r;       // request
-  uint32_t tile;    // of the request's tokens
-  uint32_t unit;    // KV head x chunk of its heads
-  uint32_t split, n_splits;
-  uint32_t slot;    // first partial result of the item's parts
-};
-
 // What is the same in every lane, into a scalar register.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -186,26 +117,6 @@ __device__ __forceinline__ float wave_total(float x) {
   return __shfl(x, 63);
 }
 
-// What a lane knows of its request: tiles of tokens, and the keys that one of
-// them can see at most.
-struct RequestWork {
-  Request q;
-  uint32_t tiles, range;
-};
-
-__device__ __forceinline__ RequestWork request_work(const AttnParams& p, uint32_t r) {
-  RequestWork w{};
-  if (r >= p.n_requests) return w;
-  w.q = request_of(p, r);
-  const uint32_t rows = w.q.rows;
-  w.tiles = (rows + p.tile_tokens - 1) / p.tile_tokens;
-  w.range = w.q.n;
-  if (p.window && !p.prefix) w.range = min(w.range, p.window + (p.tree ? rows : min(rows, p.tile_tokens)));
-  return w;
-}
-
-__device__ __forceinline__ uint32_t splits_of(uint32_t range, uint32_t part) { return range > part ? (range + part - 1) / part : 1; }
-
 __device__ __forceinline__ uint32_t wave_sum(const AttnParams& p, uint32_t x) {  // over the requests of a batch of up to 64
   return p.n_requests > 1 ? static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(wave_scan(x)), 63)) : uniform(x);
 }
@@ -237,7 +148,8 @@ __device__ __forceinline__ uint32_t part_keys(const AttnParams& p, const Request
     base = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(wave_scan(tiles)), 63)) * p.units;
     total = wave_total(total);
   }
-  const uint32_t limit = base <= p.target ? p.target : 2 * p.target;
+  // (p.parts is what the workspace holds, whatever the lengths say)
+  const uint32_t limit = lesser(base <= p.target ? p.target : 2 * p.target, p.parts);
   total *= static_cast<float>(p.units);
   if (base >= limit || (base > p.target && (p.documents || total < kLongPart * static_cast<float>(limit)))) return kWhole;
   const auto length = [&](float keys) {  // whole steps; the sum is off by less than a thousandth (2^14 additions a lane)
@@ -435,27 +347,6 @@ __device__ __forceinline__ float sum_halves(float x) {
 constexpr int kMatrix = 0x8, kLdsRead = 0x100, kVector = 0x2;
 #define BSR_ORDER(kind, n) __builtin_amdgcn_sched_group_barrier(kind, n, 0)
 
-// The bits of a row's tree mask from key offset `off` of the request's rows on,
-// ones before them.
-__device__ __forceinline__ uint64_t tree_bits(const AttnParams& p, const uint64_t* mask, int off) {
-  if (off <= -64) return ~0ull;
-  if (off < 0) return (mask[0] << -off) | ((1ull << -off) - 1);
-  const uint32_t w = off >> 6, sh = off & 63;
-  if (w >= p.tree_words) return 0;
-  uint64_t bits = mask[w] >> sh;
-  if (sh && w + 1 < p.tree_words) bits |= mask[w + 1] << (64 - sh);
-  return bits;
-}
-
-// Bits [lo, hi) of 64, both taken into 0..64.
-__device__ __forceinline__ uint64_t bit_range(int lo, int hi) {
-  lo = min(max(lo, 0), 64);
-  hi = min(max(hi, 0), 64);
-  if (lo >= hi) return 0;
-  const uint64_t to = hi == 64 ? ~0ull : (1ull << hi) - 1;
-  return to & (~0ull << lo);
-}
-
 // A wave's 32 query rows, one per lane of either half.
 struct TileRows {
   bool real;         // the row exists
@@ -606,54 +497,6 @@ __device__ void redo_row(const AttnParams& p, const Request& q, const Work& w, c
           static_cast<T>(l == 0 ? 0.0f : acc[d] / l);
   }
   if ((threadIdx.x & 63) == 0) put_stats(p, q, t, k, row, m, l);
-}
-
-// Keys [lo, hi) that a tile's rows see any of; documents are looked at by the
-// caller.
-__device__ __forceinline__ void tile_range(const AttnParams& p, const Request& q, const Work& w, int* lo, int* hi) {
-  const int i0 = w.tile * p.tile_tokens, i1 = min(i0 + static_cast<int>(p.tile_tokens), q.rows);
-  *lo = 0;
-  if (p.tree) {
-    *hi = q.n;
-    if (p.window) *lo = max(0, q.base - static_cast<int>(p.window));  // a row that sees no row stands at base - 1
-  } else {
-    *hi = q.base + i1;
-    if (p.prefix) *hi = max(*hi, min(p.prefix[w.r], q.n));
-    *hi = max(*hi, 0);
-    if (p.window) *lo = max(0, q.base + i0 - static_cast<int>(p.window) + 1);
-  }
-}
-
-// Part `split` of the keys [lo, hi): whole steps of 64 keys.
-__device__ __forceinline__ void cut(const Work& w, int lo, int hi, int* k0, int* k1) {
-  if (hi < lo) hi = lo;
-  const uint32_t len = hi - lo;
-  const uint32_t per = ((len + w.n_splits - 1) / w.n_splits + 63) & ~63u;
-  const uint64_t at = static_cast<uint64_t>(per) * w.split;
-  *k0 = at < len ? lo + static_cast<int>(at) : hi;
-  *k1 = at + per < len ? lo + static_cast<int>(at + per) : hi;
-}
-
-// The record offset of a key, and whether its block lies in the pool; keys past the
-// part's last are read as that one (the rows do not see them).
-struct KeyLoad {
-  int j;
-  uint32_t block;
-  int32_t id;
-};
-__device__ __forceinline__ KeyLoad key_load(const AttnParams& p, const Request& q, int j, int last) {
-  KeyLoad k;
-  k.j = min(j, last);
-  k.block = p.div_block.div(k.j);
-  k.id = q.table[k.block];
-  return k;
-}
-__device__ __forceinline__ bool key_offset(const AttnParams& p, const KeyLoad& k, int64_t* off) {
-  const bool ok = static_cast<uint32_t>(k.id) < p.pool_blocks;  // (fewer than 2^31)
-  const uint32_t keep = 0u - static_cast<uint32_t>(ok);  // no branch: latent steps do this beside their products
-  const uint32_t id = k.id & keep, at = (k.j - k.block * p.div_block.d) & keep;
-  *off = static_cast<int64_t>(static_cast<uint64_t>(id) * p.block_bytes + at * p.record_bytes);  // a block is smaller than 2^31 bytes
-  return ok;
 }
 
 // ---------------------------------------------------------------------------

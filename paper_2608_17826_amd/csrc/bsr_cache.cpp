@@ -87,11 +87,11 @@ int check_attn(const bsr_ctx* c, const bsr_attn_args* a, bsr::AttnParams* p) {
   if (a->k_offset + 2ull * a->n_kv_heads * a->k_dim > d.record_bytes ||
       a->v_offset + 2ull * a->n_kv_heads * a->v_dim > d.record_bytes)
     return refuse(BSR_E_ARG, "the heads reach past a record of %u bytes", d.record_bytes);
-  if (a->n_requests >= (1u << 20) || a->n_tokens >= (1u << 24) || a->max_len >= (1u << 31))
-    return refuse(BSR_E_ARG, "n_requests below 2^20, n_tokens below 2^24, max_len below 2^31");
+  if (a->n_requests >= (1u << 20) || a->n_tokens >= (1u << 24) || a->max_len >= (1u << 30) || a->window >= (1u << 30))
+    return refuse(BSR_E_ARG, "n_requests below 2^20, n_tokens below 2^24, max_len and window below 2^30");
   if (!(a->scale > 0) || !std::isfinite(a->scale)) return refuse(BSR_E_ARG, "scale must be positive and finite");
-  if (!(a->softcap >= 0) || !std::isfinite(a->softcap)) return refuse(BSR_E_ARG, "softcap must be 0, or positive and finite");
-  if (a->window >= (1u << 31)) return refuse(BSR_E_ARG, "window below 2^31");
+  if (!(a->softcap >= 0) || !std::isfinite(a->softcap) || (a->softcap > 0 && !std::isfinite(4 * (a->scale / a->softcap))))
+    return refuse(BSR_E_ARG, "softcap must be 0, or positive and finite, and so must scale / softcap");
   if (a->q_token_stride % 8 || a->q_head_stride % 8 || a->out_token_stride % 8 || a->out_head_stride % 8)
     return refuse(BSR_E_ARG, "strides must be multiples of 8 values");
   if (a->reserved) return refuse(BSR_E_ARG, "reserved must be 0");
@@ -156,6 +156,7 @@ int attend(const bsr_ctx* c, const bsr_attn_args* a, bsr::AttnParams* p, void* s
   p->units = t.units;
   p->target = t.target;
   p->min_part = t.min_part;
+  p->parts = static_cast<uint32_t>(t.slots);
   p->part = static_cast<float*>(a->workspace);
   p->part_ml = p->part + t.slots * t.tile_rows * a->v_dim;
   return enqueue(c, "attention", [&] { return bsr::launch_attention(*p, static_cast<hipStream_t>(stream)); });

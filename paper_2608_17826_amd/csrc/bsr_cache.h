@@ -90,6 +90,7 @@ struct AttnParams {
   uint32_t units;         // tiles beside one another of the same tokens: KV heads x chunks of their heads
   uint32_t target;        // parts that the batch's key ranges are cut into, about; 0: never cut
   uint32_t min_part;      // keys of a part, at least
+  uint32_t parts;         // parts that the workspace holds
   float* part;            // workspace: sums of parts [slot][tile_rows][v_dim], then their (maximum, sum)
   float* part_ml;
 };

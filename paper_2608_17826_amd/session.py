@@ -5,7 +5,8 @@ the device status block with torch, creates two default-priority streams
 (copy, compute), and drives one request at a time through bind ->
 restore_window x K -> commit.  Requests bound together under a context's
 admission budget each use a session of their own (their own ring, status
-block and streams).  All restore work runs inside libbsr.so.
+block and streams).  ``restore_into`` restores into new blocks of a
+:class:`~.cache.PagedCache`.  All restore work runs inside libbsr.so.
 """
 
 from __future__ import annotations
@@ -17,6 +18,7 @@ import numpy as np
 import torch
 
 from . import bsr
+from .cache import PagedCache
 
 
 @dataclass
@@ -124,3 +126,17 @@ class RestoreSession:
         if before_commit is not None:
             before_commit()
         return self.commit(request_id, errors)
+
+    def restore_into(self, request_id: int, n_hit: int, cache: PagedCache, row: int, **kw) -> Outcome:
+        """Restore the probed prefix into new blocks of ``cache``, as table row ``row``.
+
+        The blocks are laid out on the GPU, the other rows left alone; a prefix
+        that falls back gives them back.
+        """
+        tokens = n_hit * self.ctx.layout.chunk_tokens
+        lengths = [0] * row + [tokens]
+        cache.extend([0] * len(lengths), lengths, n_slots=tokens)
+        out = self.restore(request_id, n_hit, cache.dsts(row), **kw)
+        if out.fallback:
+            cache.release(row, tokens)
+        return out

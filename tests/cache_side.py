@@ -28,6 +28,25 @@ def ints(x, dtype=torch.int32):
     return torch.as_tensor(np.asarray(x), dtype=dtype).cuda()
 
 
+def bounds(o, l, a, dot, dtype, dk, n, bias=0.0):
+    """How far an attention row may be off: (out, lse), from what oracle.cache.attend gives.
+
+    ``n``: keys that the row sees; ``bias``: the largest distance bias.  In
+    fp32 (half a unit f = 2^-24) a score's product of dk terms is off by (dk + 8) f
+    of its sum of magnitudes, and scaling, cap, bias, log2(e), running
+    maximum and exponent round it some eight times more.  A weight is off by its
+    score's error and the maximum's, and by the exponential and the sums.  The
+    weights are rounded to the dtype (u relative; below fp16's subnormals
+    absolutely), and so is the result.
+    """
+    f, u = 2.0 ** -24, torch.finfo(dtype).eps / 2
+    ds = f * (dk + 8) * dot + 8 * f * (dot + bias)
+    dw = 2 * ds + (8 + np.log2(max(2, n)) + 64) * f
+    a = np.where(np.isfinite(a), a, 0)   # (not looked at there)
+    small = 2.0 ** -25 if dtype == torch.float16 else 0
+    return (u + dw) * a * (1 + u) + u * np.abs(o) + 1e-30 + small * (1 + a), 2 * ds + (80 + abs(l)) * 2 * f
+
+
 class AttnCase:
     """A paged cache, queries and their call.
 
@@ -153,7 +172,6 @@ class AttnCase:
         pool = self.pool.double().numpy()
         q = self.q_wide[..., :self.dk].double().numpy()
         recs = {}
-        u = torch.finfo(self.dtype).eps / 2
         worst = 0.0
         for r, i, h in todo:
             n, row = self.lens[r], int(self.starts[r]) + i
@@ -179,16 +197,10 @@ class AttnCase:
                 assert not fine.any() or l == -np.inf, where
                 np.testing.assert_array_equal(got[fine], o[fine], err_msg=where)
                 continue
-            # A score's error: its product's sum of dk terms in fp32, and six more roundings of values up to
-            # the score and its bias (scaling, cap, bias, log2(e), running maximum, exponent).
-            f = 2.0 ** -24
-            ds = f * (self.dk + 8) * dot + 8 * f * (dot + abs(slope) * len(see))
-            # a weight's relative error: its score's, the maximum's, and the exponential's (2 units) and sum's
-            dw = 2 * ds + (8 + np.log2(max(2, see.sum())) + 64) * f
-            bound = (u + dw) * a * (1 + u) + u * np.abs(o) + 1e-30 + (2.0 ** -25 if self.dtype == torch.float16 else 0) * (1 + a)
-            err, bound = np.abs(got - o)[fine], bound[fine]
+            bound, lb = bounds(o, l, a, dot, self.dtype, self.dk, int(see.sum()), abs(slope) * len(see))
+            with np.errstate(invalid="ignore"):
+                err, bound = np.abs(got - o)[fine], bound[fine]
             assert np.all(err <= bound), (where, float((err / bound).max()), got[:4], o[:4])
             worst = max(worst, float((err / bound).max(initial=0)))
-            lb = 2 * ds + (80 + abs(l)) * 2 * f
             assert abs(lse[row, h] - l) <= lb, (where, lse[row, h], l, lb)
         return worst

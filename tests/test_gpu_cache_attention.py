@@ -235,3 +235,93 @@ def test_captured_and_replayed_with_new_lengths():
         torch.cuda.synchronize()
         c.check(sample=60)
         (torch.ones(1000, device="cuda") * 2).sum().item()
+
+
+@pytest.mark.parametrize("dims,heads,kv,dtype", [(LATENT, 16, 1, "bf16"), (D128, 4, 2, "f16"), (D64, 2, 2, "bf16")])
+@pytest.mark.parametrize("n", [64, 65, 130, 700])
+def test_many_requests(dims, heads, kv, dtype, n):
+    """Batches around and past a wave's 64 requests, some without rows or tokens."""
+    rng = np.random.default_rng(n)
+    rows = rng.integers(0, 4, n)
+    lens = [int(r) + int(rng.integers(0, 400)) * int(rng.random() < 0.8) for r in rows]
+    say("case: many requests", dims, n)
+    c = AttnCase("tree", lens, rows, heads, kv, dims, dtype, block=32, masks=sum((chain(int(r)) for r in rows), []), seed=n)
+    c.run().check(sample=200)
+
+
+@pytest.mark.parametrize("dims,heads,kv", [(LATENT, 16, 1), (D128, 8, 1)])
+def test_one_long_request_among_short_ones(dims, heads, kv):
+    """Parts of one length for all: the long one's are many."""
+    lens = [50] * 30 + [20_000] + [130] * 40
+    say("case: one long request", dims)
+    c = AttnCase("tree", lens, [1] * 71, heads, kv, dims, block=64, masks=[1] * 71, seed=16).run()
+    c.check(sample=80)
+    c2 = AttnCase("tree", lens + [3] * 60, [1] * 131, heads, kv, dims, block=64, masks=[1] * 131, seed=16).run()
+    c2.check(sample=80)
+
+
+def test_more_tiles_than_the_gpu_holds_at_once():
+    """300 tiles of 128 latent heads, cut twice; the same with documents, left whole."""
+    say("case: 300 latent tiles")
+    c = AttnCase("prompt", [12_000], [300], 128, 1, LATENT, block=64, seed=17)
+    c.run().check(sample=24)
+    c.documents = [5000 + i for i in range(300)]
+    c.run().check(sample=24)
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    say("case: two streams")
+    a = AttnCase("tree", [5000, 900], [4, 2], 16, 1, LATENT, masks=chain(4) + chain(2), seed=18).place()
+    b = AttnCase("prompt", [4000], [50], 8, 2, D128, seed=19).place()
+    args = a.prepare(), b.prepare()
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        for c, x, s in zip((a, b), args, streams):
+            with torch.cuda.stream(s):
+                c.call(x)
+    torch.cuda.synchronize()
+    a.check(sample=40)
+    b.check(sample=40)
+
+
+def test_two_graphs_share_a_workspace():
+    """One after the other, with eager calls on the same workspace between."""
+    say("case: two graphs, one workspace")
+    a = AttnCase("tree", [5000, 900], [4, 2], 16, 1, LATENT, masks=chain(4) + chain(2), seed=20).place()
+    b = AttnCase("tree", [7000], [1], 16, 1, LATENT, masks=[1], seed=21).place()
+    xa, xb = a.prepare(), b.prepare()
+    big = max((xa, xb), key=lambda x: x.workspace_bytes)
+    for x in (xa, xb):
+        x.workspace, x.workspace_bytes = big.workspace, big.workspace_bytes
+    a.call(xa), b.call(xb)
+    torch.cuda.synchronize()
+    graphs = []
+    for c, x in ((a, xa), (b, xb)):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.call(x)
+        graphs.append(g)
+    for _ in range(3):
+        for c, x, g, other, y in ((a, xa, graphs[0], b, xb), (b, xb, graphs[1], a, xa)):
+            c.d["out"].fill_(7)
+            c.d["lse"].fill_(7)
+            g.replay()
+            other.call(y)
+            torch.cuda.synchronize()
+            c.check(sample=20)
+
+
+@pytest.mark.parametrize("dims,heads,kv", [(LATENT, 16, 1), (D128, 4, 2)])
+def test_blocks_past_32_bits(dims, heads, kv):
+    """Records that lie behind 2^32 bytes of their pool."""
+    say("case: blocks past 32 bits", dims)
+    c = AttnCase("tree", [700, 40], [4, 1], heads, kv, dims, masks=chain(4) + [1], seed=22).place()
+    far = (1 << 32) // (c.block * 2 * c.values) + 1
+    pool = torch.zeros((far + c.pool_blocks) * c.block, c.values, dtype=c.dtype, device="cuda")
+    pool[far * c.block:] = c.d["pool"]
+    c.d["pool"] = pool
+    c.d["tables"] = torch.where(c.d["tables"] >= 0, c.d["tables"] + far, c.d["tables"])
+    c.call(c.prepare(pool_blocks=far + c.pool_blocks))
+    torch.cuda.synchronize()
+    c.check(sample=60)
