@@ -250,7 +250,7 @@ __device__ __forceinline__ void mfma_next(f32x16& c, s16x8 a, s16x8 b) {
   if (__is_same(T, __bf16)) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
   else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
 }
-__device__ __forceinline__ void mfma_done(f32x16& c, f32x16& d) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(c), "+v"(d)); }
+__device__ __forceinline__ void mfma_done(f32x16& c) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(c)); }
 
 template <typename T>
 __device__ __forceinline__ s16x8 to_half(const float* x) {
@@ -422,12 +422,17 @@ constexpr float kRise = 8;  // the running maximum follows a rise of more than t
 // what it has summed, and the lane's factor in *back.
 template <int kSubs>
 __device__ __forceinline__ bool raise(const f32x16 (&s)[kSubs], float unit, float& m, float& l, float* back) {
-  float top = -__builtin_inff();
+  float tops[4];  // four in a row, since each waits for the last one of its own
 #pragma unroll
-  for (int u = 0; u < kSubs; ++u)
+  for (int i = 0; i < 4; ++i) tops[i] = s[0][i];
 #pragma unroll
-    for (int e = 0; e < 16; e += 2) top = fmaxf(fmaxf(top, s[u][e]), s[u][e + 1]);
-  top = max_halves(top) * unit;
+  for (int e = 4; e < 16 * kSubs; e += 8)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      tops[i] = fmaxf(tops[i], s[e / 16][e % 16 + i]);
+      if (e + 4 < 16 * kSubs) tops[i] = fmaxf(tops[i], s[(e + 4) / 16][(e + 4) % 16 + i]);
+    }
+  const float top = max_halves(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))) * unit;
   *back = 1;
   if (!__any(top > m + kRise)) return false;
   const float m1 = fmaxf(m, top);
@@ -649,7 +654,7 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) kf[i] = k_row(i % 2, i / 2);
 #pragma unroll
-    for (int i = 0; i < 2 * kN; ++i) {  // two sums in turn: a product that goes on with the last one's waits for it
+    for (int i = 0; i < 2 * kN; ++i) {
       s[i % 2] = mfma<T>(kf[i % kAhead], qf[i / 2], s[i % 2]);
       if (i + kAhead < 2 * kN) kf[i % kAhead] = k_row((i + kAhead) % 2, (i + kAhead) / 2);
     }
@@ -748,10 +753,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   // steps loaded or in use at once: three where there is LDS for no more
   constexpr int kBufs = kBlocks == 4 ? 3 : 4, kLoads = 9;  // of a wave and step
   constexpr int kKeys = kStep / 4, kIdSteps = 64 / kKeys;  // keys that a wave loads at a step; steps of one load of block ids
-  constexpr int kN = KD / 16, kAhead = 3;
+  constexpr int kN = KD / 16, kAhead = 5;
   constexpr int kHeld = kBlocks == 4 ? 32 : kN;  // products whose queries lie in registers; the others' are read from LDS
-  // Two sums in turn: a product that goes on with the last one's sum waits for it, twice as long as it takes itself.
-  constexpr int kSums = 2;
   __shared__ __attribute__((aligned(1024))) uint8_t tiles[kBufs][kTileBytes];
   __shared__ __attribute__((aligned(16))) uint8_t weights[2][kBlocks][2][1024];  // [step][rows / 32][16 keys][lane]
   __shared__ float backs[2][32 * kBlocks];
@@ -777,6 +780,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   if (lane == 0) {
     rises[0][wave] = rises[1][wave] = 0;
     redo[wave] = 0;
+    for (int i = 0; i < 8; ++i) outside[i][wave] = 0;
   }
   int lo, hi, k0, k1;
   tile_range(p, q, w, &lo, &hi);
@@ -809,14 +813,15 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
   // LDS, the others are a few instructions each).
   KeyLoad key{};
   int64_t offset = 0;
+  bool marks = false;
   auto find_offset = [&](int step, int stride) BSR_INLINE {
     if (stride == 0) key.id = block_ids[wave][step / kIdSteps & 1][step % kIdSteps * kKeys + lane % kKeys];
     if (stride == 1) key.j = key_at(step, lane % kKeys);
     if (stride == 2) key.block = p.div_block.div(key.j);
     if (stride == 3) {
-      const bool ok = key_offset(p, key, &offset);
-      // by every lane: what stands beside the products stays one block of instructions
-      outside[step & 7][wave] = static_cast<uint8_t>(~__ballot(ok));
+      const uint32_t bad = static_cast<uint8_t>(~__ballot(key_offset(p, key, &offset)));
+      marks |= bad != 0;  // nothing is written before the first block that lies outside
+      if (marks && lane == 0) outside[step & 7][wave] = static_cast<uint8_t>(bad);
     }
   };
   // load n of a step: the values of record n, or the rest of all; units of 16
@@ -857,14 +862,13 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
       return n < VD / 16 ? lds_row16(at + (k_at ^ (n % 8 * 32)) + n / 8 * 256) : lds_row16(at + (k_rest ^ ((n - VD / 16) * 32)));
     };
     s16x8 kf[kAhead], q_next{};
-    f32x16 sums[kSums];
 #pragma unroll
     for (int n = 0; n < kAhead; ++n) kf[n] = k_row(n);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int n = 0; n < kN; ++n) {
-      if (n < kSums) mfma_first<T>(sums[n], kf[n], qf[n]);
-      else mfma_next<T>(sums[n % kSums], kf[n % kAhead], n < kHeld ? qf[n < kHeld ? n : 0] : q_next);
+      if (n == 0) mfma_first<T>(s, kf[n], qf[n]);
+      else mfma_next<T>(s, kf[n % kAhead], n < kHeld ? qf[n < kHeld ? n : 0] : q_next);
       if (n + 1 >= kHeld && n + 1 < kN) q_next = *reinterpret_cast<const s16x8*>(&queries[wave][n + 1 - kHeld][lane * 16]);
       if (n + kAhead < kN) kf[n % kAhead] = k_row(n + kAhead);
       beside(n);
@@ -872,18 +876,17 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
     }
     after();
     __builtin_amdgcn_sched_barrier(0);
-    mfma_done(sums[0], sums[1]);
-    s = sums[0] + sums[1];
+    mfma_done(s);
   };
+  auto outside_of = [&](int step) BSR_INLINE { return uniform(*reinterpret_cast<const uint32_t*>(&outside[step & 7][0])); };
   // their scores, what the rows see of them, and the running maximum
-  auto settle = [&](int step, f32x16 (&s)[1], float* unit) BSR_INLINE {
+  auto settle = [&](int step, f32x16 (&s)[1], float* unit, uint32_t bad) BSR_INLINE {
     const int j0 = k0 + step * kStep;
     *unit = mods.unit;
     if (kMods) {
       *unit = 1;
       modify<kMods>(mods, t.slope2, t.see.pos, j0 + 4 * half, s[0]);
     }
-    const uint32_t bad = uniform(*reinterpret_cast<const uint32_t*>(&outside[step & 7][0]));
     if (j0 < open_lo || j0 + kStep > open_hi || bad || j0 + kStep > k1) {
       uint64_t see = bit_range(t.see.lo - j0, min(t.see.hi, k1) - j0) & ~static_cast<uint64_t>(bad);
       if (p.tree && t.real) see &= tree_bits(p, t.see.mask, j0 - q.base);
@@ -975,7 +978,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
       f32x16 s[1];
       float unit;
       score(0, s[0], [](int) {}, [] {});
-      settle(0, s, &unit);
+      settle(0, s, &unit, outside_of(0));
       leave_weights(0, s[0], unit, m > -__builtin_inff() ? m : 0.0f, 0, 16);
     }
   }
@@ -994,23 +997,25 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
       const int buf1 = buf + 1 == kBufs ? 0 : buf + 1, last = buf == 0 ? kBufs - 1 : buf - 1;
       f32x16 s[1];
       float unit;
+      const uint32_t bad = outside_of(step + 1);
       // the scores of step + 1, with the next loads beside them; then the values of this step, with the softmax of the next
       // beside them
       score(buf1, s[0], [&](int n) BSR_INLINE {
         if (n < kLoads) load_unit(n, last);
-        if (n >= 12 && n < 28 && n % 4 == 0) find_offset(step + kBufs, (n - 12) / 4);
+        if (n == 1) find_offset(step + kBufs, 0);
         if (n == kN - 3) start_values(step, buf);
       }, [&]() BSR_INLINE {
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) value_product(step, buf, i);
       });
-      settle(step + 1, s, &unit);
+      settle(step + 1, s, &unit, bad);
       const float base = m > -__builtin_inff() ? m : 0.0f;
       constexpr int kRest = kValueProducts - kBlocks;
 #pragma unroll
       for (int i = 0; i < kRest; ++i) {
         value_product(step, buf, kBlocks + i);
         leave_weights(step + 1, s[0], unit, base, i * 16 / kRest, (i + 1) * 16 / kRest);
+        if (i < 3) find_offset(step + kBufs, i + 1);
         __builtin_amdgcn_sched_barrier(0);
       }
       buf = buf1;
