@@ -570,15 +570,16 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
   const uint32_t tiles_at = lds_at(&kv_tiles[0][0][0]);
   // loading: the wave's rows of a step, kRowsPerLoad at a time
   const uint32_t load_row = wave * (kStep / 4) + lane / kUnits;
+  auto load_part = [&](int i, int buf, int64_t at) BSR_INLINE {  // load i of 2 kLoads: keys, then values of the same rows
+    const int n = i / 2;
+    const int64_t off = at + (((lane % kUnits) ^ unit_swap<D>(load_row + n * kRowsPerLoad)) * 16);
+    const uint32_t to = tiles_at + buf * (2 * kTileBytes) + (wave * (kStep / 4) + n * kRowsPerLoad) * (D * 2);
+    load_to_lds((i & 1 ? v_base : k_base) + off, to + (i & 1) * kTileBytes);
+  };
+  auto offset_at = [&](int slot, int i) BSR_INLINE { return offsets[slot][load_row + i / 2 * kRowsPerLoad]; };
   auto load_step = [&](int buf, int slot) BSR_INLINE {
 #pragma unroll
-    for (int n = 0; n < kLoads; ++n) {
-      const uint32_t r = load_row + n * kRowsPerLoad;
-      const int64_t off = offsets[slot][r] + (((lane % kUnits) ^ unit_swap<D>(r)) * 16);
-      const uint32_t to = tiles_at + buf * (2 * kTileBytes) + (wave * (kStep / 4) + n * kRowsPerLoad) * (D * 2);
-      load_to_lds(k_base + off, to);
-      load_to_lds(v_base + off, to + kTileBytes);
-    }
+    for (int i = 0; i < 2 * kLoads; ++i) load_part(i, buf, offset_at(slot, i));
   };
   KeyLoad next{}, k_first{}, k_second{};
   if (wave == 0 && steps > 0) {  // (steps past the last read its last key's block id)
@@ -619,21 +620,21 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
     v_at[e] = (v_row + 8 * e) * (D * 2) + ((v_unit ^ unit_swap<D>(v_row + 8 * e)) * 16) + (lane & 1) * 8;
 
   // waits for a step, and sends the loads of the next
-  auto turn = [&](int step) BSR_INLINE {
+  auto turn = [&](int step, bool load) BSR_INLINE {
     loads_done();
     barrier();
     const int buf = step & 1;
-    if (wave == 0 && step + 2 < steps) put_offsets(step + 2, next);
-    if (step + 1 < steps) load_step(buf ^ 1, buf ^ 1);
-    if (wave == 0 && step + 3 < steps) next = key_load(p, q, k0 + (step + 3) * kStep + lane, k1 - 1);
+    if (wave == 0) put_offsets(step + 2, next);  // (of the last key, past the last step)
+    if (load && step + 1 < steps) load_step(buf ^ 1, buf ^ 1);
+    if (wave == 0) next = key_load(p, q, k0 + (step + 3) * kStep + lane, k1 - 1);
   };
   // a wave without rows loads its share all the same (in a loop of its own: a
   // way round the sums' products would have them copied at every step)
   if (!active)
-    for (int step = 0; step < steps; ++step) turn(step);
+    for (int step = 0; step < steps; ++step) turn(step, true);
   else
   for (int step = 0; step < steps; ++step) {
-    turn(step);
+    turn(step, false);
     const int buf = step & 1, j0 = k0 + step * kStep;
     const uint32_t k_tile = tiles_at + buf * (2 * kTileBytes), v_tile = k_tile + kTileBytes;
     constexpr int kN = D / 16, kD = D / 32;
@@ -651,25 +652,23 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
     constexpr int kAhead = 4;
     f32x16 s[2] = {};
     s16x8 kf[kAhead], vf[kD];
+    int64_t off[2];
+    off[0] = offset_at(buf ^ 1, 0);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) kf[i] = k_row(i % 2, i / 2);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < 2 * kN; ++i) {
       s[i % 2] = mfma<T>(kf[i % kAhead], qf[i / 2], s[i % 2]);
       if (i + kAhead < 2 * kN) kf[i % kAhead] = k_row((i + kAhead) % 2, (i + kAhead) / 2);
-    }
-#pragma unroll
-    for (int d = 0; d < kD; ++d) vf[d] = v_cols(0, d);
-    BSR_ORDER(kLdsRead, kAhead);
-#pragma unroll
-    for (int i = 0; i < 2 * kN - kAhead; ++i) {
-      BSR_ORDER(kMatrix, 1);
-      BSR_ORDER(kLdsRead, 1);
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      BSR_ORDER(kMatrix, 1);
-      BSR_ORDER(kLdsRead, 2);
+      else if (i + kAhead - 2 * kN < kD) vf[i + kAhead - 2 * kN] = v_cols(0, i + kAhead - 2 * kN);
+      // the next step's loads (past the last step, of its last key's record), one
+      // beside every second product: a load holds its wave up
+      if (i % 2 == 0 && i / 2 < 2 * kLoads) {
+        load_part(i / 2, buf ^ 1, off[i / 4 % 2]);
+        if (i % 4 == 0 && i / 4 + 1 < kLoads) off[(i / 4 + 1) % 2] = offset_at(buf ^ 1, i / 2 + 2);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
     float unit = mods.unit;
     if (kMods) {
@@ -709,6 +708,7 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
     }
   }
 
+  loads_done();  // none may reach LDS that is no longer the workgroup's
   const Sink sink{w.n_splits > 1, w.slot + w.split};
   l = sum_halves(l);
   const float inv = sink.part ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
