@@ -1215,8 +1215,8 @@ AttnTiling attn_tiling(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
   const uint32_t per_kv = n_heads / n_kv_heads;
   t.tile_heads = per_kv < kTileRows ? per_kv : kTileRows;
   t.tile_rows = kTileRows;
-  if (v_dim == 512 && n_requests && n_tokens % n_requests == 0) {
-    // requests of as many rows each, it seems: no more row blocks than those need
+  if (v_dim == 512 && n_requests && n_tokens && n_tokens % n_requests == 0) {
+    // requests of as many rows each, it seems (and at least one): no more row blocks than those need
     const uint64_t rows = static_cast<uint64_t>(n_tokens) / n_requests * t.tile_heads;
     t.tile_rows = rows <= 32 ? 32 : rows <= 64 ? 64 : kTileRows;
   }

@@ -92,6 +92,14 @@ def test_workspace_bytes(ctx):
     assert code(bsr.bsr_attn_workspace_bytes, ctx, attn(scale=0.0)) == bsr.BSR_E_ARG
 
 
+@pytest.mark.parametrize("n_requests", [0, 1, 2])
+@pytest.mark.parametrize("heads", [1, 16, 33, 128, 300])
+def test_workspace_bytes_without_rows(ctx, heads, n_requests):
+    """More heads than the smallest tile has rows, and no rows at all."""
+    assert bsr.bsr_attn_workspace_bytes(ctx, attn(n_heads=heads, n_requests=n_requests, n_tokens=0, max_len=1 << 20)) == 0
+    assert code(bsr.bsr_attend_tree, ctx, attn(n_heads=heads, n_requests=n_requests, n_tokens=0)) == bsr.BSR_E_DEVICE
+
+
 def append(**other):
     f = dict(group=0, n_tokens=3, slots=A, pool=A, pool_blocks=4, src_type=bsr.BSR_TYPE_BF16,
              cache_type=bsr.BSR_TYPE_BF16, sources=[(A, 512, 512), (A, 64, 64)])
