@@ -97,7 +97,7 @@ def test_workspace_bytes(ctx):
 def test_workspace_bytes_without_rows(ctx, heads, n_requests):
     """More heads than the smallest tile has rows, and no rows at all."""
     assert bsr.bsr_attn_workspace_bytes(ctx, attn(n_heads=heads, n_requests=n_requests, n_tokens=0, max_len=1 << 20)) == 0
-    assert code(bsr.bsr_attend_tree, ctx, attn(n_heads=heads, n_requests=n_requests, n_tokens=0)) == bsr.BSR_E_DEVICE
+    assert code(bsr.bsr_attend_tree, ctx, attn(n_heads=heads, n_requests=n_requests, n_tokens=0), 0) == bsr.BSR_E_DEVICE
 
 
 def append(**other):
