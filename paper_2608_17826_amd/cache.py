@@ -80,6 +80,9 @@ class PagedCache:
     def blocks(self, g: int, tokens: int) -> int:
         return -(-tokens // self.groups[g].block_tokens)
 
+    def _check_row(self, row: int) -> None:
+        _check(0 <= row < self.max_requests, f"table row {row} of {self.max_requests}")
+
     # ---- block tables --------------------------------------------------------------
     def extend(self, cached: Sequence[int], added: Sequence[int], n_slots: Optional[int] = None) -> Batch:
         """Blocks and slots for ``added[r]`` more tokens of request r (table row r), which holds ``cached[r]``.
@@ -116,6 +119,9 @@ class PagedCache:
 
     def release(self, row: int, tokens: int) -> None:
         """Puts the blocks of ``tokens`` tokens of table row ``row`` behind the free ones."""
+        self._check_row(row)
+        _check(tokens >= 0 and all(self.blocks(g, tokens) <= t.shape[1] for g, t in enumerate(self.tables)),
+               "more blocks than a table holds")
         for g in range(len(self.groups)):
             n = self.blocks(g, tokens)
             self.free[g] = torch.cat([self.free[g][self.taken[g]:], self.tables[g][row, :n]])
@@ -123,6 +129,7 @@ class PagedCache:
 
     def dsts(self, row: int) -> List[bsr.bsr_group_dst]:
         """Destinations of a restore into table row ``row`` (for bsr_request_bind)."""
+        self._check_row(row)
         return [bsr.group_dst(tab.data_ptr() + 4 * row * tab.shape[1], base.data_ptr(), v.data_ptr(), tab.shape[1], n)
                 for tab, base, v, n in zip(self.tables, self.bases, self.valid, self.pool_blocks)]
 
@@ -159,6 +166,10 @@ class PagedCache:
             out = torch.empty(n, heads, dims[1], dtype=q.dtype, device=self.device)
         _check(tuple(out.shape) == (n, heads, dims[1]) and out.dtype == q.dtype and out.device == self.device and
                out.stride(2) == 1, f"out is [tokens, heads, {dims[1]}] of q's type")
+        for x, size in ((batch.starts, batch.lens.numel() + 1), (batch.lens, batch.lens.numel())):
+            _check(x.dtype == torch.int32 and x.is_contiguous() and x.device == self.device and x.numel() == size,
+                   "a batch's starts and lens are int32 [n_requests + 1] and [n_requests]")
+        _check(batch.lens.numel() <= self.max_requests, "the batch has more requests than the tables have rows")
         sums = torch.empty(n, heads, dtype=torch.float32, device=self.device) if lse else None
         for x, dtype, size in arrays.values():
             _check(x is None or (x.dtype == dtype and x.is_contiguous() and x.device == self.device and x.numel() == size),

@@ -131,12 +131,14 @@ class RestoreSession:
         """Restore the probed prefix into new blocks of ``cache``, as table row ``row``.
 
         The blocks are laid out on the GPU, the other rows left alone; a prefix
-        that falls back gives them back.
+        that falls back gives them back (an exception does not: the GPU may still
+        write to them).
         """
         tokens = n_hit * self.ctx.layout.chunk_tokens
+        dsts = cache.dsts(row)
         lengths = [0] * row + [tokens]
         cache.extend([0] * len(lengths), lengths, n_slots=tokens)
-        out = self.restore(request_id, n_hit, cache.dsts(row), **kw)
+        out = self.restore(request_id, n_hit, dsts, **kw)
         if out.fallback:
             cache.release(row, tokens)
         return out

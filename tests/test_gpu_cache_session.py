@@ -14,7 +14,7 @@ from cache_side import bounds
 from gpu_side import layout_of, say
 from oracle import cache as oracle_cache
 from paper_2608_17826_amd import bsr
-from paper_2608_17826_amd.cache import PagedCache
+from paper_2608_17826_amd.cache import Batch, PagedCache
 from paper_2608_17826_amd.session import RestoreSession
 from workloads import generate
 from workloads.configs import GroupSpec, Workload
@@ -208,6 +208,33 @@ def test_captured_decode_step():
             check_rows(o, lse, q, k, k[:, :512], [0], lambda i: oracle_cache.visible("tree", at + 1, 1, 0, mask=[1]),
                        float(np.float32(576 ** -0.5)))
         bsr.bsr_request_end(e.ctx, 9)
+    finally:
+        bsr.bsr_ctx_destroy(e.ctx)
+
+
+def test_the_cache_checks_rows_and_batches():
+    """Rows outside the tables, blocks that a row cannot hold, and batches that are not the tables'."""
+    e = Engine()
+    c = e.cache
+    try:
+        b = c.extend([0], [4])
+        before = [t.clone() for t in c.tables], list(c.taken)
+        q = torch.zeros(4, 2, 128, dtype=torch.bfloat16, device="cuda")
+        i32 = dict(dtype=torch.int32, device="cuda")
+        attend = lambda starts, lens: c.attend_prompt(2, (0, 0), q, Batch(starts, lens, b.slots, b.result),  # noqa: E731
+                                                      (128, 128), 1, 600, (0, 256))
+        say("case: rows and batches that are not the cache's")
+        for call in [lambda: c.dsts(-1), lambda: c.dsts(3), lambda: c.release(3, 4), lambda: c.release(-1, 4),
+                     lambda: c.release(0, -1), lambda: c.release(0, 601 + 16), lambda: e.session.restore_into(5, 1, c, -1),
+                     lambda: e.session.restore_into(5, 1, c, 3),
+                     lambda: attend(torch.zeros(5, **i32), torch.zeros(4, **i32)), lambda: attend(b.starts[:1], b.lens),
+                     lambda: attend(b.starts.long(), b.lens), lambda: attend(b.starts, b.lens.long()),
+                     lambda: attend(b.starts.cpu(), b.lens), lambda: attend(torch.zeros(4, **i32)[::2], b.lens)]:
+            with pytest.raises(bsr.BsrError) as x:
+                call()
+            assert x.value.code == bsr.BSR_E_ARG
+        assert c.taken == before[1] and all(torch.equal(a, t) for a, t in zip(before[0], c.tables))
+        attend(b.starts, b.lens)
     finally:
         bsr.bsr_ctx_destroy(e.ctx)
 
