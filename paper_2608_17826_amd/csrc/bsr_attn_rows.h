@@ -3,8 +3,6 @@
 // that a CPU test checks them.
 #pragma once
 
-#include <algorithm>
-
 #include "bsr_cache.h"
 
 #define BSR_ROWS_FN __host__ __device__ __forceinline__
@@ -106,6 +104,12 @@ struct Work {
   uint32_t split, n_splits;
   uint32_t slot;    // first partial result of the item's parts
 };
+
+// Whether an item's parts lie in the workspace and can be joined.  Always, but
+// for starts that decrease: their tiles may number past 32 bits.
+BSR_ROWS_FN bool parts_fit(const AttnParams& p, const Work& w) {
+  return w.n_splits < 2 || (w.n_splits <= p.parts && w.n_splits <= kMaxTarget && w.slot <= p.parts - w.n_splits);
+}
 
 // What a lane knows of its request: tiles of tokens, and the keys that one of
 // them can see at most.

@@ -283,7 +283,7 @@ __global__ __launch_bounds__(kAppendThreads) void k_append_scaled128(AppendParam
 #pragma unroll
   for (int d = 8; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
   const float scale = most < __builtin_inff() ? most / 448.0f : __builtin_nanf("");
-  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(4)));  // (a block of an odd number of tokens)
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = scaled(x[i], scale);
   *reinterpret_cast<u32x2*>(to.values + lane * 8) = u32x2{pack_e4m3(x[0], x[1], x[2], x[3]), pack_e4m3(x[4], x[5], x[6], x[7])};

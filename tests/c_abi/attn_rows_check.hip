@@ -122,6 +122,16 @@ int main() {
       }
     }
   }
+  // items whose parts the workspace holds, and no others, whatever the sums wrapped to
+  for (int number = 0; number < 4000; ++number) {
+    AttnParams p{};
+    p.parts = pick(0, 3) ? pick(0, 2 * kMaxTarget) : 0;
+    Work w{};
+    w.n_splits = pick(0, 3) ? pick(1, 2 * kMaxTarget) : static_cast<uint32_t>(rng()) | 1;
+    w.slot = pick(0, 3) ? pick(0, 2 * kMaxTarget) : static_cast<uint32_t>(rng());
+    const uint64_t end = static_cast<uint64_t>(w.slot) + w.n_splits;
+    EXPECT(parts_fit(p, w) == (w.n_splits == 1 || (end <= p.parts && w.n_splits <= kMaxTarget)));
+  }
   std::puts("ok");
   return 0;
 }

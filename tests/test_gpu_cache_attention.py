@@ -117,6 +117,16 @@ def test_prompt_masks(dims, heads, kv, what):
     c.run().check(sample=400)
 
 
+@pytest.mark.parametrize("dims,heads,kv,dtype", [(D128, 4, 2, "f16"), (D64, 2, 1, "bf16"), (LATENT, 16, 1, "f16")])
+@pytest.mark.parametrize("cap,scale", [(63.0, None), (65.0, None), (65.0, 4.0), (1e4, None), (1e6, 40.0), (1e30, None),
+                                       (3e38, 1e-3), (1e-30, None)])
+def test_caps_of_every_width(dims, heads, kv, dtype, cap, scale):
+    """Caps far above the scores leave them alone; scores on both sides of 0.4 caps; a cap that leaves them all zero."""
+    say("case: caps", dims, cap, scale)
+    c = AttnCase("prompt", [150, 40], [70, 1], heads, kv, dims, dtype, cap=cap, scale=scale, seed=12)
+    c.run().check(sample=200)
+
+
 def test_more_rows_than_tokens():
     """Rows before the first position see nothing (of a prompt), or what the tree still has."""
     say("case: more rows than tokens")
