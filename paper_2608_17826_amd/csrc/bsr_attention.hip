@@ -254,6 +254,7 @@ __device__ __forceinline__ void mfma_next(f32x16& c, s16x8 a, s16x8 b) {
   else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void mfma_done(f32x16& c) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(c)); }
+__device__ __forceinline__ void mfma_done(f32x16& a, f32x16& b) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(a), "+v"(b)); }
 
 template <typename T>
 __device__ __forceinline__ s16x8 to_half(const float* x) {
@@ -391,6 +392,7 @@ struct ScoreMods {
   float cap2;       // softcap x log2(e), 0 without
   float in_cap;     // 2 log2(e) scale / softcap: tanh(x) = 1 - 2 / (2^(2 x log2 e) + 1)
   float over;       // scale / softcap where the cap is wide, else 0
+  bool ahead;       // rows see keys behind their own position
 };
 // That tanh is off by 2^-23 or so however small x is, which a cap c makes c 2^-23 or
 // more of a score: from here on scores below 0.4 c take the first terms of its
@@ -404,12 +406,12 @@ __device__ __forceinline__ ScoreMods score_mods(const AttnParams& p) {
   m.cap2 = p.softcap * kLog2e;
   m.in_cap = p.softcap > 0 ? 2 * kLog2e * (p.scale / p.softcap) : 0;
   m.over = p.softcap > kWideCap ? p.scale / p.softcap : 0;
+  m.ahead = p.prefix != nullptr;
   return m;
 }
 
 template <int kMods>
 __device__ __forceinline__ void modify(const ScoreMods& m, float slope2, int pos, int j0, f32x16& s) {
-  const float away = static_cast<float>(pos - j0);
   if (kMods & kCap) {
     if (m.cap2 > kWideCap * kLog2e) {
 #pragma unroll
@@ -422,22 +424,40 @@ __device__ __forceinline__ void modify(const ScoreMods& m, float slope2, int pos
         const float x = s[e] * m.unit;
         const float far = m.cap2 - 2 * m.cap2 * __builtin_amdgcn_rcpf(exp2_(s[e] * m.in_cap) + 1);
         s[e] = fabsf(z) < 0.4f ? __builtin_fmaf(x, z2 * y, x) : far;
+        if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (all at once take more registers than there are)
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = m.cap2 - 2 * m.cap2 * __builtin_amdgcn_rcpf(exp2_(s[e] * m.in_cap) + 1);
+      for (int e = 0; e < 16; ++e) {
+        s[e] = m.cap2 - 2 * m.cap2 * __builtin_amdgcn_rcpf(exp2_(s[e] * m.in_cap) + 1);
+        if (e % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
+  if (!(kMods & kSlopes)) return;
+  const float unit = kMods & kCap ? 1.0f : m.unit, away = static_cast<float>(pos - j0);
+  if (m.ahead) {
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    float x = s[e];
-    if (!(kMods & kCap)) x *= m.unit;
-    if (kMods & kSlopes) x = __builtin_fmaf(-slope2, fabsf(away - static_cast<float>(8 * (e / 4) + e % 4)), x);
-    s[e] = x;
+    for (int e = 0; e < 16; ++e)
+      s[e] = __builtin_fmaf(-slope2, fabsf(away - static_cast<float>(8 * (e / 4) + e % 4)), s[e] * unit);
+  } else {  // two instructions a score: the distance of a key that is seen has one sign
+    const float from = -slope2 * away;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      s[e] = __builtin_fmaf(s[e], unit, __builtin_fmaf(slope2, static_cast<float>(8 * (e / 4) + e % 4), from));
   }
 }
 
 constexpr float kRise = 8;  // the running maximum follows a rise of more than this (weights up to 2^8 until then)
+
+// The compiler's own maximum first multiplies each operand by one, against a
+// signalling NaN: a third of the instructions here (rows that meet a NaN are done again).  It sees no
+// result of a matrix product here: mfma_done or modify comes before.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float x;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(a), "v"(b), "v"(c));
+  return x;
+}
 
 // The running maximum m and sum l of a lane's row after 16 kSubs more scores
 // (`unit` is what is left to multiply them by).  Returns whether any row of the wave rescales
@@ -446,15 +466,15 @@ template <int kSubs>
 __device__ __forceinline__ bool raise(const f32x16 (&s)[kSubs], float unit, float& m, float& l, float* back) {
   float tops[4];  // four in a row, since each waits for the last one of its own
 #pragma unroll
-  for (int i = 0; i < 4; ++i) tops[i] = s[0][i];
+  for (int i = 0; i < 4; ++i) tops[i] = max3(s[0][i], s[0][4 + i], s[0][8 + i]);
 #pragma unroll
-  for (int e = 4; e < 16 * kSubs; e += 8)
+  for (int e = 12; e < 16 * kSubs; e += 8)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      tops[i] = fmaxf(tops[i], s[e / 16][e % 16 + i]);
-      if (e + 4 < 16 * kSubs) tops[i] = fmaxf(tops[i], s[(e + 4) / 16][(e + 4) % 16 + i]);
+      const int n = e + 4 < 16 * kSubs ? e + 4 : e;
+      tops[i] = max3(tops[i], s[e / 16][e % 16 + i], s[n / 16][n % 16 + i]);
     }
-  const float top = max_halves(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))) * unit;
+  const float top = max_halves(fmaxf(max3(tops[0], tops[1], tops[2]), tops[3])) * unit;
   *back = 1;
   if (!__any(top > m + kRise)) return false;
   const float m1 = fmaxf(m, top);
@@ -473,6 +493,12 @@ __device__ __forceinline__ float weigh(f32x16& s, float unit, float from) {
     sum[e & 1] += s[e];
   }
   return sum[0] + sum[1];
+}
+
+// A score where bit n of `see` is set, else -infinity.
+__device__ __forceinline__ float seen(float s, uint32_t see, int n) {
+  const int keep = static_cast<int>(see << (31 - n)) >> 31;
+  return __uint_as_float((__float_as_uint(s) & keep) | (0xff800000u & ~keep));
 }
 
 // Where a tile's row goes: the output, or a partial result.
@@ -693,7 +719,9 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
       __builtin_amdgcn_sched_barrier(0);
     }
     float unit = mods.unit;
-    if (kMods) {
+    if (!kMods) {
+      mfma_done(s[0], s[1]);
+    } else {
       unit = 1;
 #pragma unroll
       for (int u = 0; u < 2; ++u) modify<kMods>(mods, t.slope2, t.see.pos, j0 + 32 * u + 4 * half, s[u]);
@@ -707,7 +735,7 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (!(see >> (32 * u + 8 * (e / 4) + e % 4) & 1)) s[u][e] = -__builtin_inff();
+          s[u][e] = seen(s[u][e], static_cast<uint32_t>(see >> (32 * u)), 8 * (e / 4) + e % 4);
     }
     float back;
     if (raise<2>(s, unit, m, l, &back)) {
@@ -915,7 +943,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
       see >>= 4 * half;
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (!(see >> (8 * (e / 4) + e % 4) & 1)) s[0][e] = -__builtin_inff();
+        s[0][e] = seen(s[0][e], static_cast<uint32_t>(see), 8 * (e / 4) + e % 4);
     }
     float back;
     const bool rise = raise<1>(s, *unit, m, l, &back);
