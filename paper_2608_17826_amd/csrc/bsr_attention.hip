@@ -582,13 +582,13 @@ __device__ void redo_row(const AttnParams& p, const Request& q, const Work& w, c
 //
 // Heads of 128 leave registers for 2 workgroups a CU, heads of 64 for 3.  What
 // bounds it: with many rows the matrix and the vector unit in turn (a step's 32
-// products of a wave take 1,090 cycles, its 64 scores a lane 1,150 without mask,
+// products of a wave take 1,090 cycles, its 32 scores a lane some 900 without mask,
 // cap or bias), and the clock, 1.8 GHz under this load; with few rows the cache's
 // bytes.  1,024 tokens of 16 heads behind 128K: 1,100-1,170 us, 940-1,000
 // TFLOP/s; one token of 32 heads over 128K: 112 us, 4.8 TB/s; 8 trees of 64
 // nodes, 32 heads, capped, over 9,000: 52 us (the cap's exponential and reciprocal
-// are half of the vector unit's time), 4,096 and fewer packed tokens of 16 heads
-// of 64 with a bias: 50 us (4 to 5 steps a tile, behind 6 us to the first).
+// are as many cycles as the rest of the softmax); 10.7K packed tokens of 16 heads
+// of 64 with a bias: 50 us (5.4 steps a tile, behind some 6 us to the first).
 // ---------------------------------------------------------------------------
 constexpr int kAttnThreads = 256;
 
@@ -819,7 +819,7 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
 // The sums of 128 rows are 256 accumulator registers, so a CU holds one
 // workgroup; tiles of 32 or 64 rows (kBlocks 1, 2) score with one or two waves and
 // have a buffer more.  What bounds it: a step of 128 rows takes 5,000 cycles, of
-// which the products 2,170; a load holds its wave 80 cycles, 9 of them a step, and
+// which the products 2,310; a load holds its wave 80 cycles, 9 of them a step, and
 // the softmax of a step has only the products of the step before beside it.  4
 // nodes of 128 heads over 512K: 590-610 us, 960-990 TFLOP/s; 16 trees of 8 nodes, 16
 // heads, over up to 33K: 79 us, 3.3 TB/s; one token of 16 heads over 1,000: 12.3
