@@ -711,7 +711,8 @@ uint64_t bsr_attn_workspace_bytes(bsr_ctx* ctx, const bsr_attn_args* args);
  * is refused.  slopes, prefix and documents must be NULL.
  *
  * Here and below: sums, the softmax and lse are in fp32, the weights are
- * rounded to dtype for the products with the values, and out is rounded once.
+ * rounded to dtype for the products with the values (fp16's, besides, to 2^-31
+ * of their sum), and out is rounded once.
  * A row that sees no key gets zeros and lse = -infinity.  Keys that a row does not
  * see count for nothing, whatever they hold, infinities and NaN included.  Blocks whose id lies
  * outside [0, pool_blocks) are not read and not seen. */

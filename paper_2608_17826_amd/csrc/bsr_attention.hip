@@ -455,11 +455,21 @@ __device__ __forceinline__ void modify(const ScoreMods& m, float slope2, int pos
   }
 }
 
-// The running maximum follows a rise of more than this (weights up to 2^8 until
-// then, which the sums in fp32 and the weights in 16 bits hold alike): past a
-// row's first steps its sums are rescaled hardly ever.  Following every rise: 16
-// latent trees of 8 nodes 179 us for 94, causal 8192 382 for 372.
+// The running maximum m follows a rise of more than kRise (weights grow by up to
+// 2^8 until then, which the sums in fp32 and the weights in 16 bits hold alike):
+// past a row's first steps its sums are rescaled hardly ever.  Following every
+// rise: 16 latent trees of 8 nodes 179 us for 94, causal 8192 382 for 372.
+//
+// m is the maximum less kLift, so that the largest weight is 2^kLift.  fp16's
+// weights are rounded to steps of 2^-24 at the least: with 1 for the largest, a key
+// below half of one would count for nothing, though enough of them matter (each off by
+// 2^-25 of the sum, 2^17 of them by 2^-8).  With 2^7 to 2^15 (65,504 is the
+// type's most) a key is off by 2^-32 of the sum, 2^20 of them by 2^-12.  The same
+// trees in fp16: 87 us with a lift of 0 or 7; 90 with a lift of 9 and a
+// rise of 6, 100 with 11 and 4, which leave less.
 constexpr float kRise = 8;
+template <typename T>
+constexpr float kLift = __is_same(T, _Float16) ? 7 : 0;
 
 // The compiler's own maximum first multiplies each operand by one, against a
 // signalling NaN: half of the instructions of a maximum (rows that meet a NaN are
@@ -474,7 +484,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // The running maximum m and sum l of a lane's row after 16 kSubs more scores
 // (`unit` is what is left to multiply them by).  Returns whether any row of the
 // wave rescales what it has summed, and the lane's factor in *back.
-template <int kSubs>
+template <typename T, int kSubs>
 __device__ __forceinline__ bool raise(const f32x16 (&s)[kSubs], float unit, float& m, float& l, float* back) {
   float tops[4];  // four in a row, since each waits for the last one of its own
 #pragma unroll
@@ -488,8 +498,8 @@ __device__ __forceinline__ bool raise(const f32x16 (&s)[kSubs], float unit, floa
     }
   const float top = max_halves(fmaxf(max3(tops[0], tops[1], tops[2]), tops[3])) * unit;
   *back = 1;
-  if (!__any(top > m + kRise)) return false;
-  const float m1 = fmaxf(m, top);
+  if (!__any(top > m + (kLift<T> + kRise))) return false;
+  const float m1 = fmaxf(m, top - kLift<T>);
   *back = m > -__builtin_inff() ? exp2_(m - m1) : 0.0f;
   l *= *back;
   m = m1;
@@ -761,7 +771,7 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
           s[u][e] = seen(s[u][e], static_cast<uint32_t>(see >> (32 * u)), 8 * (e / 4) + e % 4);
     }
     float back;
-    if (raise<2>(s, unit, m, l, &back)) {
+    if (raise<T, 2>(s, unit, m, l, &back)) {
 #pragma unroll
       for (int d = 0; d < kD; ++d) o[d] *= back;
     }
@@ -979,7 +989,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
         s[0][e] = seen(s[0][e], static_cast<uint32_t>(see), 8 * (e / 4) + e % 4);
     }
     float back;
-    const bool rise = raise<1>(s, *unit, m, l, &back);
+    const bool rise = raise<T, 1>(s, *unit, m, l, &back);
     if (rise && half == 0) backs[step & 1][row] = back;
     if (lane == 0) rises[step & 1][wave] = rise;
   };
