@@ -130,15 +130,28 @@ class RestoreSession:
     def restore_into(self, request_id: int, n_hit: int, cache: PagedCache, row: int, **kw) -> Outcome:
         """Restore the probed prefix into new blocks of ``cache``, as table row ``row``.
 
-        The blocks are laid out on the GPU, the other rows left alone; a prefix
-        that falls back gives them back (an exception does not: the GPU may still
-        write to them).
+        The blocks are laid out on the GPU, the other rows left alone.  A prefix
+        that falls back gives them back, and so does a request whose bind is
+        refused (e.g. BSR_E_BUSY: it may be tried again).  An exception after the
+        bind does not: the GPU may still write to them until the request has ended.
         """
         tokens = n_hit * self.ctx.layout.chunk_tokens
         dsts = cache.dsts(row)
         lengths = [0] * row + [tokens]
         cache.extend([0] * len(lengths), lengths, n_slots=tokens)
-        out = self.restore(request_id, n_hit, dsts, **kw)
+        bound, after_bind = False, kw.pop("after_bind", None)
+
+        def on_bind():
+            nonlocal bound
+            bound = True
+            if after_bind is not None:
+                after_bind()
+        try:
+            out = self.restore(request_id, n_hit, dsts, after_bind=on_bind, **kw)
+        except Exception:
+            if not bound:
+                cache.release(row, tokens)
+            raise
         if out.fallback:
             cache.release(row, tokens)
         return out
