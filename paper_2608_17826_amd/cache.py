@@ -57,6 +57,7 @@ class PagedCache:
         self.device = pools[0][0].device
         self.groups = [L.groups[g] for g in range(L.n_groups)]
         self.pool_blocks, self.bases, self.valid, self.tables, self.free, self.taken = [], [], [], [], [], []
+        self._valid = []       # valid, and a byte more for block ids outside the pool
         for g, (d, ts) in enumerate(zip(self.groups, self.pools)):
             _check(len(ts) == d.n_tensors, f"group {g} has {d.n_tensors} tensors")
             n = ts[0].shape[0]
@@ -66,7 +67,8 @@ class PagedCache:
                        f"group {g}: a pool is a contiguous uint8 [pool_blocks, {d.block_tokens * d.record_bytes}] tensor")
             self.pool_blocks.append(n)
             self.bases.append(torch.tensor([t.data_ptr() for t in ts], dtype=torch.int64, device=self.device))
-            self.valid.append(torch.zeros(n, dtype=torch.uint8, device=self.device))
+            self._valid.append(torch.zeros(n + 1, dtype=torch.uint8, device=self.device))
+            self.valid.append(self._valid[g][:n])
             self.tables.append(torch.full((max_requests, -(-max_tokens // d.block_tokens)), -1, dtype=torch.int32,
                                           device=self.device))
             ids = torch.arange(n, dtype=torch.int32, device=self.device) if free is None else free[g]
@@ -118,13 +120,18 @@ class PagedCache:
         return b
 
     def release(self, row: int, tokens: int) -> None:
-        """Puts the blocks of ``tokens`` tokens of table row ``row`` behind the free ones."""
+        """Puts the blocks of ``tokens`` tokens of table row ``row`` behind the free ones.
+
+        They read as not valid from then on, until a restore commits into them.
+        """
         self._check_row(row)
         _check(tokens >= 0 and all(self.blocks(g, tokens) <= t.shape[1] for g, t in enumerate(self.tables)),
                "more blocks than a table holds")
         for g in range(len(self.groups)):
-            n = self.blocks(g, tokens)
-            self.free[g] = torch.cat([self.free[g][self.taken[g]:], self.tables[g][row, :n]])
+            ids = self.tables[g][row, :self.blocks(g, tokens)]
+            n = self.pool_blocks[g]
+            self._valid[g].index_fill_(0, torch.where((ids >= 0) & (ids < n), ids, n).long(), 0)
+            self.free[g] = torch.cat([self.free[g][self.taken[g]:], ids])
             self.taken[g] = 0
 
     def dsts(self, row: int) -> List[bsr.bsr_group_dst]:

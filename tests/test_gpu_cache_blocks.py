@@ -6,6 +6,7 @@ import torch
 
 from gpu_side import say
 from paper_2608_17826_amd import bsr
+from paper_2608_17826_amd.cache import PagedCache
 from test_gpu_cache_session import W, Engine
 
 pytestmark = [pytest.mark.gpu, pytest.mark.timeout(300)]
@@ -77,3 +78,36 @@ def test_a_hook_that_raises_keeps_the_blocks(engine):
     bsr.bsr_invalidate(e.ctx, 23, bsr.BSR_FAIL_ABORT)
     bsr.bsr_commit(e.ctx, 23)
     bsr.bsr_request_end(e.ctx, 23)
+
+
+def test_released_blocks_are_not_valid(engine):
+    """Blocks of a restored prefix that hold something else next."""
+    e, c = engine, engine.cache
+    n, _, _ = bsr.bsr_probe(e.ctx, 24, e.wi.salt, e.wi.tokens)
+    e.session.restore_into(24, n, c, row=2)
+    bsr.bsr_request_end(e.ctx, 24)
+    b = c.extend([0, 0, 320], [50, 0, 9])
+    assert [int(v.sum()) for v in c.valid] == [c.blocks(g, 320) for g in range(3)]
+    say("case: a restored request ends")
+    c.release(2, 329)
+    assert not any(v.any() for v in c.valid)
+    c.extend([50], [500])
+    assert not any(v.any() for v in c.valid)
+    assert b.result.tolist()[0] == 3
+
+
+def test_block_ids_outside_the_pool_are_released_too(engine):
+    """As many as a list of free ids has; nothing is written for them."""
+    e = engine
+    say("case: free ids outside the pool")
+    free = [torch.tensor([90, 3, -1, 2 ** 31 - 1, 89, 0], dtype=torch.int32, device="cuda") for _ in W.groups]
+    c = PagedCache(e.ctx, e.cache.pools, max_requests=2, max_tokens=600, free=free)
+    for v in c.valid:
+        v.fill_(1)
+    c.extend([0], [32])     # 2, 1 and 4 blocks
+    c.release(0, 32)
+    got = [v.cpu().numpy() for v in c.valid]
+    for v, ids in zip(got, ([90, 3], [90], [90, 3, -1, 2 ** 31 - 1])):
+        want = np.ones(90, np.uint8)
+        want[[i for i in ids if 0 <= i < 90]] = 0
+        np.testing.assert_array_equal(v, want)
