@@ -44,8 +44,11 @@ class PagedCache:
 
     ``pools[g][t]``: uint8 tensor of tensor t of group g, [pool_blocks, block
     bytes].  ``free[g]``: int32 ids of the group's free blocks, all of them by
-    default.  The cache takes blocks from the front of ``free`` and never puts
-    any back by itself (:meth:`release`).
+    default.  The cache takes blocks from the front of ``free`` and puts them
+    back behind the others: at :meth:`release`, and where :meth:`extend` is given fewer
+    tokens than a row's blocks were laid out for (drafted ones that were rejected).
+    ``held[g][row]``: how many blocks of group g a table row holds; a program
+    that moves rows of ``tables`` moves these with them.
     """
 
     def __init__(self, ctx: bsr.Ctx, pools: Sequence[Sequence[torch.Tensor]], max_requests: int, max_tokens: int,
@@ -57,6 +60,7 @@ class PagedCache:
         self.device = pools[0][0].device
         self.groups = [L.groups[g] for g in range(L.n_groups)]
         self.pool_blocks, self.bases, self.valid, self.tables, self.free, self.taken = [], [], [], [], [], []
+        self.held = [[0] * max_requests for _ in self.groups]
         self._valid = []       # valid, and a byte more for block ids outside the pool
         for g, (d, ts) in enumerate(zip(self.groups, self.pools)):
             _check(len(ts) == d.n_tensors, f"group {g} has {d.n_tensors} tensors")
@@ -86,26 +90,46 @@ class PagedCache:
         _check(0 <= row < self.max_requests, f"table row {row} of {self.max_requests}")
 
     # ---- block tables --------------------------------------------------------------
-    def extend(self, cached: Sequence[int], added: Sequence[int], n_slots: Optional[int] = None) -> Batch:
-        """Blocks and slots for ``added[r]`` more tokens of request r (table row r), which holds ``cached[r]``.
+    def _give_back(self, g: int, ids: Sequence[torch.Tensor]) -> None:
+        """Block ids behind the free ones; they read as not valid until a restore commits into them."""
+        ids = torch.cat(list(ids))
+        n = self.pool_blocks[g]
+        self._valid[g].index_fill_(0, torch.where((ids >= 0) & (ids < n), ids, n).long(), 0)
+        self.free[g] = torch.cat([self.free[g][self.taken[g]:], ids])
+        self.taken[g] = 0
 
-        Raises where the free blocks or a table do not hold all of them, before
-        anything is enqueued.
+    def extend(self, cached: Sequence[int], added: Sequence[int], n_slots: Optional[int] = None) -> Batch:
+        """Blocks and slots for ``added[r]`` more tokens of request r (table row r), which has ``cached[r]``.
+
+        A row that gets tokens first gives back the blocks that it holds behind
+        the cached ones'; a row that gets none is left alone.  Raises where a row
+        does not hold its cached tokens' blocks, or the free blocks or a table have no room
+        for all of them, before anything is enqueued.
         """
         n = len(cached)
         _check(n <= self.max_requests and len(added) == n and all(c >= 0 and a >= 0 for c, a in zip(cached, added)),
                "lengths of up to max_requests requests, none negative")
         n_slots = sum(added) if n_slots is None else n_slots
         _check(sum(added) <= n_slots, "n_slots is fewer than the new tokens")
-        take = []
+        rows = [r for r in range(n) if added[r]]
+        take, back = [], []
         for g in range(len(self.groups)):
-            need = [self.blocks(g, c + a) for c, a in zip(cached, added)]
-            take.append(sum(need) - sum(self.blocks(g, c) for c in cached))
-            if max(need, default=0) > self.tables[g].shape[1]:
+            have, held = {r: self.blocks(g, cached[r]) for r in rows}, self.held[g]
+            need = {r: self.blocks(g, cached[r] + added[r]) for r in rows}
+            for r in rows:
+                _check(have[r] <= held[r], f"group {g}: table row {r} holds {held[r]} blocks, fewer than {cached[r]} tokens")
+            take.append(sum(need.values()) - sum(have.values()))
+            back.append([(r, have[r], held[r]) for r in rows if have[r] < held[r]])
+            if max(need.values(), default=0) > self.tables[g].shape[1]:
                 raise bsr.BsrError(bsr.BSR_E_ARG, f"group {g}: a request outgrows its table")
-            if self.taken[g] + take[g] > self.free[g].numel():
-                raise bsr.BsrError(bsr.BSR_E_NOMEM, f"group {g}: {take[g]} blocks wanted, "
-                                   f"{self.free[g].numel() - self.taken[g]} free")
+            left = self.free[g].numel() - self.taken[g] + sum(to - at for _, at, to in back[g])
+            if take[g] > left:
+                raise bsr.BsrError(bsr.BSR_E_NOMEM, f"group {g}: {take[g]} blocks wanted, {left} free")
+        for g, rests in enumerate(back):
+            if rests:
+                self._give_back(g, [self.tables[g][r, at:to] for r, at, to in rests])
+                for r, at, _ in rests:
+                    self.held[g][r] = at
         i32 = dict(dtype=torch.int32, device=self.device)
         lengths = torch.tensor([list(cached), list(added)], dtype=torch.int32, pin_memory=True).to(self.device, non_blocking=True)
         b = Batch(torch.empty(n + 1, **i32), torch.empty(n, **i32),
@@ -117,22 +141,24 @@ class PagedCache:
                                                        b.starts.data_ptr(), b.lens.data_ptr(), b.result.data_ptr()),
                              self._stream())
         self.taken = [t + k for t, k in zip(self.taken, take)]
+        for g, held in enumerate(self.held):
+            for r in rows:
+                held[r] = self.blocks(g, cached[r] + added[r])
         return b
 
     def release(self, row: int, tokens: int) -> None:
-        """Puts the blocks of ``tokens`` tokens of table row ``row`` behind the free ones.
+        """The request of table row ``row``, of ``tokens`` tokens, is over: all blocks of the row go behind the free ones.
 
-        They read as not valid from then on, until a restore commits into them.
+        (Those of drafted tokens that it did not keep among them.)  Raises where
+        the row holds fewer blocks than its tokens take, so where it was released before.
         """
         self._check_row(row)
-        _check(tokens >= 0 and all(self.blocks(g, tokens) <= t.shape[1] for g, t in enumerate(self.tables)),
-               "more blocks than a table holds")
-        for g in range(len(self.groups)):
-            ids = self.tables[g][row, :self.blocks(g, tokens)]
-            n = self.pool_blocks[g]
-            self._valid[g].index_fill_(0, torch.where((ids >= 0) & (ids < n), ids, n).long(), 0)
-            self.free[g] = torch.cat([self.free[g][self.taken[g]:], ids])
-            self.taken[g] = 0
+        _check(tokens >= 0 and all(self.blocks(g, tokens) <= held[row] for g, held in enumerate(self.held)),
+               f"table row {row} does not hold {tokens} tokens")
+        for g, held in enumerate(self.held):
+            if held[row]:
+                self._give_back(g, [self.tables[g][row, :held[row]]])
+                held[row] = 0
 
     def dsts(self, row: int) -> List[bsr.bsr_group_dst]:
         """Destinations of a restore into table row ``row`` (for bsr_request_bind)."""

@@ -128,15 +128,18 @@ class RestoreSession:
         return self.commit(request_id, errors)
 
     def restore_into(self, request_id: int, n_hit: int, cache: PagedCache, row: int, **kw) -> Outcome:
-        """Restore the probed prefix into new blocks of ``cache``, as table row ``row``.
+        """Restore the probed prefix into new blocks of ``cache``, as table row ``row``, which holds none.
 
         The blocks are laid out on the GPU, the other rows left alone.  A prefix
         that falls back gives them back, and so does a request whose bind is
         refused (e.g. BSR_E_BUSY: it may be tried again).  An exception after the
-        bind does not: the GPU may still write to them until the request has ended.
+        bind does not: the GPU may still write to them until the request has ended,
+        and then the row can be released.
         """
         tokens = n_hit * self.ctx.layout.chunk_tokens
         dsts = cache.dsts(row)
+        if any(held[row] for held in cache.held):
+            raise bsr.BsrError(bsr.BSR_E_ARG, f"table row {row} holds blocks: release them first")
         lengths = [0] * row + [tokens]
         cache.extend([0] * len(lengths), lengths, n_slots=tokens)
         bound, after_bind = False, kw.pop("after_bind", None)

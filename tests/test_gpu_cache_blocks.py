@@ -111,3 +111,96 @@ def test_block_ids_outside_the_pool_are_released_too(engine):
         want = np.ones(90, np.uint8)
         want[[i for i in ids if 0 <= i < 90]] = 0
         np.testing.assert_array_equal(v, want)
+
+
+def check_whole(c, tokens):
+    """Every block id is free or one row's, once; the rows hold what their tokens need."""
+    for g in range(len(W.groups)):
+        held = [c.tables[g][r, :c.blocks(g, n)].tolist() for r, n in enumerate(tokens)]
+        assert sorted(sum(held, free_ids(c)[g])) == list(range(90)), g
+
+
+def test_rejected_drafts_keep_no_blocks(engine):
+    """A tree's tokens of which the next call keeps fewer."""
+    c = engine.cache
+    say("case: drafts rejected")
+    c.extend([0], [7])
+    for at in (7, 8, 9, 10, 13, 16, 30, 31, 64):
+        c.extend([at], [40])
+        check_whole(c, [at + 40])
+        c.extend([at], [1 if at != 30 else 0])     # (a request that adds nothing is left alone)
+        check_whole(c, [at + (1 if at != 30 else 40)])
+        if at != 64:
+            c.extend([at], [40])
+    say("case: none kept")
+    c.extend([0], [3])
+    check_whole(c, [3])
+    c.release(0, 1)     # the request ends: the blocks of what it did not keep go too
+    check_whole(c, [0])
+
+
+def test_blocks_given_back_are_there_to_take(engine):
+    c = engine.cache
+    say("case: the pool's last blocks")
+    c.extend([0, 0], [8, 600])      # 1 + 75 of the last group's 90 blocks
+    c.release(1, 600)
+    c.extend([0, 0], [0, 560])
+    c.extend([8], [8 * 19])         # 1 + 19 + 70: all of them
+    assert free_ids(c)[2] == []
+    before = [t.clone() for t in c.tables], list(c.taken), free_ids(c)
+    assert code(lambda: c.extend([8 * 20], [1])) == bsr.BSR_E_NOMEM
+    assert code(lambda: c.extend([8, 560], [8 * 19, 1])) == bsr.BSR_E_NOMEM
+    assert all(torch.equal(a, t) for a, t in zip(before[0], c.tables)) and (c.taken, free_ids(c)) == before[1:]
+    b = c.extend([8, 560], [8 * 18, 1])     # the first gives 19 back and takes 18
+    assert b.result.tolist()[0] == 2
+    check_whole(c, [8 * 19, 561])
+
+
+def test_rows_that_do_not_hold_what_a_call_says(engine):
+    """A second release, a release or a request of more than a row holds, a restore into a row in use."""
+    e, c = engine, engine.cache
+    n, _, _ = bsr.bsr_probe(e.ctx, 25, e.wi.salt, e.wi.tokens)
+    c.extend([0, 0], [5, 40])
+    say("case: rows that do not hold what a call says")
+    for call in (lambda: c.release(0, 9), lambda: c.release(2, 1), lambda: c.extend([0, 0, 1], [0, 0, 1]),
+                 lambda: c.extend([17, 40], [1, 1]), lambda: e.session.restore_into(25, n, c, row=1)):
+        assert code(call) == bsr.BSR_E_ARG
+        check_whole(c, [5, 40])
+    c.release(0, 5)
+    for call in (lambda: c.release(0, 5), lambda: c.release(0, 1), lambda: c.extend([5], [1])):
+        assert code(call) == bsr.BSR_E_ARG
+        check_whole(c, [0, 40])
+    c.release(0, 0)
+    c.release(1, 40)
+    check_whole(c, [0, 0])
+    out = e.session.restore_into(25, n, c, row=1)
+    assert out.exposed_tokens == 320
+    check_whole(c, [0, 320])
+    bsr.bsr_request_end(e.ctx, 25)
+
+
+def test_blocks_through_random_calls(engine):
+    c = engine.cache
+    rng = np.random.default_rng(7)
+    tokens = [0, 0, 0]      # that the rows' blocks were laid out for
+    say("case: random calls")
+    for step in range(60):
+        if rng.random() < 0.25:
+            r = int(rng.integers(3))
+            c.release(r, int(rng.integers(tokens[r] + 1)))
+            tokens[r] = 0
+        else:
+            k = int(rng.integers(1, 4))
+            cached = [int(rng.integers(max(0, t - 30), t + 1)) for t in tokens[:k]]
+            added = [int(rng.integers(0, 70)) for _ in range(k)]
+            then = [x + y if y else t for x, y, t in zip(cached, added, tokens)] + tokens[k:]
+            if max(then) > 600 or any(sum(c.blocks(g, t) for t in then) > 90 for g in range(3)):
+                continue
+            b = c.extend(cached, added)
+            tokens = then
+            assert b.result.tolist()[0] == k
+            for g, s in enumerate(W.groups):
+                want = [int(c.tables[g][r, p // s.block_tokens]) * s.block_tokens + p % s.block_tokens
+                        for r in range(k) for p in range(cached[r], cached[r] + added[r])]
+                assert b.slots[g].tolist() == want
+        check_whole(c, tokens)
