@@ -669,7 +669,7 @@ typedef struct bsr_attn_args {
   const void* q;         /* [n_tokens][n_heads][k_dim], 16-byte aligned; strides in values, multiples of 8,
                             the last dimension contiguous */
   int64_t q_token_stride, q_head_stride;
-  void* out;             /* [n_tokens][n_heads][v_dim], likewise */
+  void* out;             /* [n_tokens][n_heads][v_dim], likewise; no two rows overlap */
   int64_t out_token_stride, out_head_stride;
   float* lse;            /* fp32 [n_tokens][n_heads]: natural logarithm of the sum of exp(score); may be NULL */
   const void* k_pool;    /* pools of pool_blocks blocks, 16-byte aligned; KV head g of a token lies at */

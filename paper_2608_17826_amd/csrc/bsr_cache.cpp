@@ -69,6 +69,25 @@ bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
 
 bool aligned(const void* p, uint64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+// Whether rows of `width` values that begin at t * st + h * sh (t < nt, h < nh) overlap.
+bool rows_overlap(int64_t st, int64_t nt, int64_t sh, int64_t nh, int64_t width) {
+  if (nt < 1 || nh < 1) return false;
+  const __int128 at = st < 0 ? -static_cast<__int128>(st) : st, ah = sh < 0 ? -static_cast<__int128>(sh) : sh;
+  // one within the other, as tensors and their views have it
+  if ((nt == 1 || at >= (nh - 1) * ah + width) && (nh == 1 || ah >= width)) return false;
+  if ((nh == 1 || ah >= (nt - 1) * at + width) && (nt == 1 || at >= width)) return false;
+  // any other two strides: for each distance of heads the distances of tokens that come closest
+  for (int64_t dh = 0; dh < nh; ++dh) {
+    const __int128 h = static_cast<__int128>(dh) * sh, near = st ? -h / st : 0;
+    for (int i = -1; i <= 1; ++i) {
+      const __int128 dt = near + i < 1 - nt ? 1 - nt : near + i > nt - 1 ? nt - 1 : near + i;
+      const __int128 gap = dt * st + h;
+      if ((dt || dh) && gap < width && -gap < width) return true;
+    }
+  }
+  return false;
+}
+
 int check_attn(const bsr_ctx* c, const bsr_attn_args* a, bsr::AttnParams* p) {
   const bsr_layout* L = bsr::ctx_layout(c);
   if (a->group >= L->n_groups) return refuse(BSR_E_ARG, "group %u of %u", a->group, L->n_groups);
@@ -106,6 +125,8 @@ int check_attn(const bsr_ctx* c, const bsr_attn_args* a, bsr::AttnParams* p) {
       return refuse(BSR_E_ARG, "an array is not aligned to its type");
     if (a->pool_blocks == 0 || a->pool_blocks >= (1u << 31)) return refuse(BSR_E_ARG, "pool_blocks must be in 1..2^31-1");
     if (a->table_stride == 0) return refuse(BSR_E_ARG, "table_stride is 0");
+    if (rows_overlap(a->out_token_stride, a->n_tokens, a->out_head_stride, a->n_heads, a->v_dim))
+      return refuse(BSR_E_ARG, "rows of out overlap");
   }
   p->q = static_cast<const uint8_t*>(a->q);
   p->out = static_cast<uint8_t*>(a->out);

@@ -1,0 +1,45 @@
+"""Limits of the paged cache's operators, from either side (CPU).
+
+A host-only context is enough: a call with good arguments gets as far as
+BSR_E_DEVICE.  Addresses are made up; nothing is read through them.
+"""
+
+import random
+
+import pytest
+
+from paper_2608_17826_amd import bsr
+from test_lib_cache import HEADS, attn, code, ctx  # noqa: F401  (ctx: the fixture)
+
+
+def attend_code(ctx, **other):  # noqa: F811
+    codes = {code(call, ctx, attn(mode, **other), 0) for mode, call in (("tree", bsr.bsr_attend_tree),
+                                                                        ("prompt", bsr.bsr_attend_prompt))}
+    assert len(codes) == 1
+    return codes.pop()
+
+
+@pytest.mark.parametrize("strides,tokens,heads,fine", [
+    ((1024, 128), 5, 8, True), ((0, 128), 1, 8, True), ((0, 128), 2, 8, False), ((1024, 0), 5, 1, True),
+    ((1024, 0), 5, 8, False), ((0, 0), 1, 1, True), ((1016, 128), 2, 8, False), ((1024, 120), 1, 8, False),
+    ((128, 640), 5, 8, True), ((128, 632), 5, 8, False), ((-1024, 128), 5, 8, True), ((1024, -128), 5, 8, True),
+    ((-1016, -128), 5, 8, False), ((256, 384), 2, 2, True), ((256, 384), 4, 8, False), ((256, 384), 3, 2, True),
+    ((256, 384), 4, 3, False), ((1 << 60, 1 << 60), 2, 8, False), ((1 << 60, 128), 5, 8, True),
+    ((-(1 << 60), 1 << 56), 15, 8, True), ((-(1 << 60), 1 << 56), 17, 17, False)])
+def test_rows_of_out_that_overlap(ctx, strides, tokens, heads, fine):  # noqa: F811
+    got = attend_code(ctx, **dict(HEADS, n_heads=heads, n_tokens=tokens, out_strides=strides))
+    assert got == (bsr.BSR_E_DEVICE if fine else bsr.BSR_E_ARG), bsr.bsr_last_error()
+
+
+def test_rows_of_out_that_overlap_by_the_definition(ctx):  # noqa: F811
+    rng = random.Random(3)
+    seen = set()
+    for _ in range(400):
+        tokens, heads = rng.randint(1, 6), rng.randint(1, 6)
+        strides = tuple(8 * rng.randint(-70, 70) for _ in range(2))
+        at = sorted(t * strides[0] + h * strides[1] for t in range(tokens) for h in range(heads))
+        fine = all(b - a >= 128 for a, b in zip(at, at[1:]))
+        seen.add(fine)
+        got = attend_code(ctx, **dict(HEADS, n_heads=heads, n_tokens=tokens, out_strides=strides))
+        assert got == (bsr.BSR_E_DEVICE if fine else bsr.BSR_E_ARG), (strides, tokens, heads)
+    assert seen == {True, False}
