@@ -632,7 +632,8 @@ int bsr_tables_build(bsr_ctx* ctx, const bsr_tables_args* args, void* stream);
 
 typedef struct bsr_append_args {
   uint32_t group;        /* of the context's layout */
-  uint32_t n_tokens;     /* rows; 0 does nothing */
+  uint32_t n_tokens;     /* rows, < 2^24; 0 does nothing.  CONTIG: together fewer than 2^32 - 256 values, or units
+                            of 8 where all of source, widths, strides and record are whole 16-byte units */
   const int64_t* slots;  /* int64[n_tokens]: block * block_tokens + position; rows whose slot lies outside
                             [0, pool_blocks * block_tokens) are skipped.  No slot twice */
   void* pool;            /* one tensor's pool, 16-byte aligned */
@@ -662,8 +663,11 @@ typedef struct bsr_attn_args {
   uint32_t dtype;       /* of q, out and the cache: BSR_TYPE_BF16 or F16 */
   uint32_t n_requests;  /* < 2^20; 0 does nothing */
   uint32_t n_tokens;    /* < 2^24: rows of q, out, lse; those at starts[n_requests] and after stay as they are */
-  uint32_t n_heads;     /* a multiple of n_kv_heads */
-  uint32_t n_kv_heads;
+  uint32_t n_heads;     /* 1..4096, a multiple of n_kv_heads */
+  uint32_t n_kv_heads;  /* With R rows a tile (128; 32 or 64 where latent requests have that few rows and heads
+                           each), k = min(n_heads / n_kv_heads, 128) and t = R / k tokens of a tile, tiles number
+                           n_kv_heads * ceil(n_heads / n_kv_heads / k) * (n_tokens / t + min(n_requests, n_tokens)),
+                           < 2^24 */
   uint32_t k_dim, v_dim; /* (64, 64), (128, 128), or (576, 512): latent records, one KV head, whose value is
                             the first 512 of the key (v_pool = k_pool, v_offset = k_offset) */
   const void* q;         /* [n_tokens][n_heads][k_dim], 16-byte aligned; strides in values, multiples of 8,

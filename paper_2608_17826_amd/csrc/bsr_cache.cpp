@@ -164,13 +164,18 @@ bsr::AttnTiling tiling_of(const bsr_attn_args* a) {
   return bsr::attn_tiling(a->n_requests, a->n_tokens, a->n_heads, a->n_kv_heads, a->v_dim, a->max_len);
 }
 
+int check_tiling(const bsr::AttnTiling& t) {
+  if (t.items >= (1ull << 24)) return refuse(BSR_E_ARG, "too many rows and heads for one launch");
+  return BSR_OK;
+}
+
 int attend(const bsr_ctx* c, const bsr_attn_args* a, bsr::AttnParams* p, void* stream) {
   if (a->n_requests == 0 || a->n_tokens == 0) return check_device(c);
   const bsr::AttnTiling t = tiling_of(a);
+  if (int rc = check_tiling(t)) return rc;
   if (t.workspace && (!a->workspace || !aligned(a->workspace, 16) || a->workspace_bytes < t.workspace))
     return refuse(BSR_E_ARG, "workspace is NULL, not 16-byte aligned or smaller than %llu bytes",
                   static_cast<unsigned long long>(t.workspace));
-  if (t.items >= (1ull << 24)) return refuse(BSR_E_ARG, "too many rows and heads for one launch");
   p->tile_rows = t.tile_rows;
   p->tile_heads = t.tile_heads;
   p->tile_tokens = t.tile_tokens;
@@ -280,7 +285,8 @@ int bsr_cache_append(bsr_ctx* c, const bsr_append_args* a, void* stream) {
 
 uint64_t bsr_attn_workspace_bytes(bsr_ctx* c, const bsr_attn_args* a) {
   if (check_ctx(c, a) || check_attn(c, a, nullptr)) return BSR_ATTN_REFUSED;
-  return tiling_of(a).workspace;
+  const bsr::AttnTiling t = tiling_of(a);
+  return check_tiling(t) ? BSR_ATTN_REFUSED : t.workspace;
 }
 
 int bsr_attend_tree(bsr_ctx* c, const bsr_attn_args* a, void* stream) {

@@ -43,3 +43,17 @@ def test_rows_of_out_that_overlap_by_the_definition(ctx):  # noqa: F811
         got = attend_code(ctx, **dict(HEADS, n_heads=heads, n_tokens=tokens, out_strides=strides))
         assert got == (bsr.BSR_E_DEVICE if fine else bsr.BSR_E_ARG), (strides, tokens, heads)
     assert seen == {True, False}
+
+
+@pytest.mark.parametrize("tokens,heads,fine", [
+    (1 << 23, 256, False), ((1 << 23) - 3, 256, True), ((1 << 24) - 1, 128, False), ((1 << 24) - 3, 128, True),
+    ((1 << 24) - 1, 64, True)])
+def test_too_many_tiles(ctx, tokens, heads, fine):  # noqa: F811
+    """The workspace's size is refused where the call is."""
+    other = dict(HEADS, n_tokens=tokens, n_heads=heads, out_strides=(heads * 128, 128))
+    assert attend_code(ctx, **other) == (bsr.BSR_E_DEVICE if fine else bsr.BSR_E_ARG)
+    if fine:
+        assert bsr.bsr_attn_workspace_bytes(ctx, attn(**other)) >= 0
+    else:
+        assert code(bsr.bsr_attn_workspace_bytes, ctx, attn(**other)) == bsr.BSR_E_ARG
+        assert bsr.bsr_last_error()
