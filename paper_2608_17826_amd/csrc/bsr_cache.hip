@@ -17,18 +17,15 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // LDS, so one launch does and nothing is handed from workgroup to workgroup.
 // A wave takes every fourth sum, a lane the requests of 1/64 of the batch, so a
 // sum is one scan within the wave and the waves meet once.  Sums saturate at
-// 2^31 - 1, which no admitted request reaches (n_slots and n_free are smaller).
+// 2^32 - 1, which no admitted request reaches (n_slots and n_free are below 2^31).
 // Then a thread finds its row's request by bisection and writes its slot in every
 // group; the row that is the first of a block writes the block's table entry.
 // ---------------------------------------------------------------------------
 constexpr int kTablesThreads = 256;
-constexpr uint32_t kSat = 0x7fffffffu;
+constexpr uint32_t kMostTokens = 0x7fffffffu;
 __device__ const int32_t kNoBlock = 0;
 
-__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) {
-  const uint32_t s = a + b;  // both at most 2^31 - 1
-  return s < kSat ? s : kSat;
-}
+__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 
 template <int kCtrl, int kRows>
 __device__ __forceinline__ uint32_t sat_step(uint32_t x) {
@@ -56,7 +53,7 @@ struct Lengths {
 };
 __device__ __forceinline__ Lengths lengths_of(const TablesBuildParams& p, int32_t c, int32_t a) {
   Lengths x;
-  x.fits = c >= 0 && a >= 0 && static_cast<uint32_t>(c) + static_cast<uint32_t>(a) <= kSat;
+  x.fits = c >= 0 && a >= 0 && static_cast<uint32_t>(c) + static_cast<uint32_t>(a) <= kMostTokens;
   for (uint32_t g = 0; g < p.n_groups; ++g)
     if (p.g[g].tables && x.fits && blocks_of(p.g[g].div_block, c + a) > p.g[g].table_stride) x.fits = false;
   x.have = x.fits ? c : 0;
