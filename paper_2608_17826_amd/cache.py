@@ -110,7 +110,7 @@ class PagedCache:
         _check(n <= self.max_requests and len(added) == n and all(c >= 0 and a >= 0 for c, a in zip(cached, added)),
                "lengths of up to max_requests requests, none negative")
         n_slots = sum(added) if n_slots is None else n_slots
-        _check(sum(added) <= n_slots, "n_slots is fewer than the new tokens")
+        _check(sum(added) <= n_slots < 1 << 31, "n_slots is fewer than the new tokens, or not below 2^31")
         rows = [r for r in range(n) if added[r]]
         take, back = [], []
         for g in range(len(self.groups)):
@@ -194,6 +194,8 @@ class PagedCache:
                 out, lse: bool):
         _check(q.dim() == 3 and q.dtype in (torch.bfloat16, torch.float16) and q.device == self.device and
                q.stride(2) == 1 and q.shape[2] == dims[0], f"q is [tokens, heads, {dims[0]}] of bfloat16 or float16")
+        _check(all(0 <= x < 1 << 32 for x in (group, kv_heads, max_len, window, *offsets)),
+               "group, kv_heads, max_len, window and offsets are of 32 bits")
         n, heads, _ = q.shape
         if out is None:
             out = torch.empty(n, heads, dims[1], dtype=q.dtype, device=self.device)
