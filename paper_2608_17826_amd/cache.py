@@ -39,6 +39,11 @@ def _check(ok: bool, what: str) -> None:
         raise bsr.BsrError(bsr.BSR_E_ARG, what)
 
 
+def _check_no_grad(*tensors: Optional[torch.Tensor]) -> None:
+    _check(not (torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in tensors)),
+           "append and attention have no backward pass: detach the tensors, or call under torch.no_grad()")
+
+
 class PagedCache:
     """Pools and block tables of a batch of up to ``max_requests`` requests of ``max_tokens`` tokens.
 
@@ -180,6 +185,7 @@ class PagedCache:
             _check(s.dim() == 2 and s.shape[0] == n and s.dtype == x.dtype and s.device == self.device and
                    (s.stride(1) == 1 or s.shape[1] == 1), "sources are [n, width] rows of one type")
         _check(x.dtype in _TYPES, "sources are bfloat16, float16 or float32")
+        _check_no_grad(*sources)
         planar = self.groups[group].kind == bsr.BSR_KIND_PLANAR
         dtype = torch.bfloat16 if dtype is None else dtype
         _check(planar or dtype in (torch.bfloat16, torch.float16), "a cache holds bfloat16 or float16")
@@ -194,6 +200,7 @@ class PagedCache:
                 out, lse: bool):
         _check(q.dim() == 3 and q.dtype in (torch.bfloat16, torch.float16) and q.device == self.device and
                q.stride(2) == 1 and q.shape[2] == dims[0], f"q is [tokens, heads, {dims[0]}] of bfloat16 or float16")
+        _check_no_grad(q, out, *(x for x, _, _ in arrays.values()))
         _check(all(0 <= x < 1 << 32 for x in (group, kv_heads, max_len, window, *offsets)),
                "group, kv_heads, max_len, window and offsets are of 32 bits")
         n, heads, _ = q.shape

@@ -49,3 +49,21 @@ def test_numbers_past_32_bits_are_refused(engine):
     before = list(c.taken)
     assert code(lambda: c.extend([0, 0], [0, 1], n_slots=2 ** 32 + 1)) == bsr.BSR_E_ARG
     assert c.taken == before and c.held[2][1] == 0
+
+
+def test_gradients_are_refused(engine):
+    c = engine.cache
+    b, kv, q = new_tokens(c)
+    say("case: gradients")
+    c.append(2, 0, b.slots[2], [kv])
+    out = attend(c, q, b)
+    one = torch.ones(4, 1, dtype=torch.int64, device="cuda")
+    leaf, rows = q.clone().requires_grad_(), kv.clone().requires_grad_()
+    for call in (lambda: attend(c, leaf, b), lambda: attend(c, leaf * 1, b), lambda: c.append(2, 0, b.slots[2], [rows]),
+                 lambda: attend(c, q, b, slopes=torch.zeros(2, device="cuda").requires_grad_()),
+                 lambda: c.attend_tree(2, (0, 0), leaf, b, one, (128, 128), 1, 600, (0, 256))):
+        assert code(call) == bsr.BSR_E_ARG
+    with torch.no_grad():
+        c.append(2, 0, b.slots[2], [rows])
+        assert torch.equal(attend(c, leaf, b), out)
+    assert torch.equal(attend(c, leaf.detach(), b), out)
