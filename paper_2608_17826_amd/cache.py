@@ -15,7 +15,7 @@ Shapes and types of tensors are checked here, everything else by the library.
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import List, Optional, Sequence, Tuple
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import torch
 
@@ -53,7 +53,9 @@ class PagedCache:
     back behind the others: at :meth:`release`, and where :meth:`extend` is given fewer
     tokens than a row's blocks were laid out for (drafted ones that were rejected).
     ``held[g][row]``: how many blocks of group g a table row holds; a program
-    that moves rows of ``tables`` moves these with them.
+    that moves rows of ``tables`` moves these with them.  ``types[g, t]``: what
+    :meth:`append` has written into tensor t of group g, bfloat16 or float16; only
+    that is appended to it or read as such from then on.
     """
 
     def __init__(self, ctx: bsr.Ctx, pools: Sequence[Sequence[torch.Tensor]], max_requests: int, max_tokens: int,
@@ -66,6 +68,7 @@ class PagedCache:
         self.groups = [L.groups[g] for g in range(L.n_groups)]
         self.pool_blocks, self.bases, self.valid, self.tables, self.free, self.taken = [], [], [], [], [], []
         self.held = [[0] * max_requests for _ in self.groups]
+        self.types: Dict[Tuple[int, int], torch.dtype] = {}
         self._valid = []       # valid, and a byte more for block ids outside the pool
         for g, (d, ts) in enumerate(zip(self.groups, self.pools)):
             _check(len(ts) == d.n_tensors, f"group {g} has {d.n_tensors} tensors")
@@ -171,6 +174,11 @@ class PagedCache:
         return [bsr.group_dst(tab.data_ptr() + 4 * row * tab.shape[1], base.data_ptr(), v.data_ptr(), tab.shape[1], n)
                 for tab, base, v, n in zip(self.tables, self.bases, self.valid, self.pool_blocks)]
 
+    def _check_type(self, group: int, tensor: int, dtype: torch.dtype) -> Tuple[int, int]:
+        key = group, tensor % len(self.pools[group])
+        _check(self.types.get(key, dtype) == dtype, f"group {group}: tensor {tensor} holds {self.types.get(key)}")
+        return key
+
     # ---- append -----------------------------------------------------------------------
     def append(self, group: int, tensor: int, slots: torch.Tensor, sources: Sequence[torch.Tensor],
                dtype: Optional[torch.dtype] = None) -> None:
@@ -189,10 +197,13 @@ class PagedCache:
         planar = self.groups[group].kind == bsr.BSR_KIND_PLANAR
         dtype = torch.bfloat16 if dtype is None else dtype
         _check(planar or dtype in (torch.bfloat16, torch.float16), "a cache holds bfloat16 or float16")
+        key = None if planar else self._check_type(group, tensor, dtype)
         a = bsr.append_args(group, n, slots.data_ptr(), self.pools[group][tensor].data_ptr(), self.pool_blocks[group],
                             _TYPES[x.dtype], bsr.BSR_TYPE_E4M3_SCALED if planar else _TYPES[dtype],
                             [(s.data_ptr(), s.shape[1], max(s.stride(0), s.shape[1]) if n < 2 else s.stride(0)) for s in sources])
         bsr.bsr_cache_append(self.ctx, a, self._stream())
+        if key is not None:
+            self.types[key] = dtype
 
     # ---- attention -----------------------------------------------------------------------
     def _attend(self, call, group: int, tensors: Tuple[int, int], q: torch.Tensor, batch: Batch, dims, kv_heads: int,
@@ -216,6 +227,8 @@ class PagedCache:
         for x, dtype, size in arrays.values():
             _check(x is None or (x.dtype == dtype and x.is_contiguous() and x.device == self.device and x.numel() == size),
                    "a mask's array has another type or size")
+        for t in tensors:
+            self._check_type(group, t, q.dtype)
         tab = self.tables[group]
         ptr = lambda x: 0 if x is None else x.data_ptr()  # noqa: E731
         a = bsr.attn_args(group=group, dtype=_TYPES[q.dtype], n_requests=batch.lens.numel(), n_tokens=n, n_heads=heads,

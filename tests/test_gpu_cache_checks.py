@@ -67,3 +67,23 @@ def test_gradients_are_refused(engine):
         c.append(2, 0, b.slots[2], [rows])
         assert torch.equal(attend(c, leaf, b), out)
     assert torch.equal(attend(c, leaf.detach(), b), out)
+
+
+@pytest.mark.parametrize("dtype,other", [(torch.bfloat16, torch.float16), (torch.float16, torch.bfloat16)])
+def test_a_cache_read_or_written_as_another_type(engine, dtype, other):
+    c = engine.cache
+    b, kv, q = new_tokens(c, dtype=dtype)
+    say("case: another type than the cache's", dtype)
+    attend(c, q, b), attend(c, q.to(other), b)      # nothing has been appended: either may be what was restored
+    c.append(2, 0, b.slots[2], [kv], dtype=dtype)
+    out = attend(c, q, b)
+    assert code(lambda: attend(c, q.to(other), b)) == bsr.BSR_E_ARG
+    assert code(lambda: c.append(2, 0, b.slots[2], [kv], dtype=other)) == bsr.BSR_E_ARG
+    c.append(2, 0, b.slots[2], [kv.float()], dtype=dtype)    # (the source's type is another matter)
+    assert torch.equal(attend(c, q, b), out)
+    x = torch.zeros(4, 576, device="cuda")
+    c.append(0, 0, b.slots[0], [x], dtype=other)     # another tensor
+    c.append(0, 1, b.slots[0], [x], dtype=dtype)
+    c.types.pop((2, 0))                              # the pool starts over
+    c.append(2, 0, b.slots[2], [kv], dtype=other)
+    attend(c, q.to(other), b)
