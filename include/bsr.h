@@ -723,7 +723,9 @@ uint64_t bsr_attn_workspace_bytes(bsr_ctx* ctx, const bsr_attn_args* args);
 int bsr_attend_tree(bsr_ctx* ctx, const bsr_attn_args* args, void* stream);
 
 /* Attention of prompt tokens.  With p = n - T + i, row i sees keys j with
- * j <= p or j < min(prefix, n), j > p - window if there is one, and j >= documents[row].  tree must be NULL. */
+ * j <= p or j < min(prefix, n), j > p - window if there is one, and j >= documents[row].  tree must be NULL.
+ * A prefix is the request's, not a document's: rows of a document before its end see all keys up to there, those
+ * of later documents among them.  Documents that see nothing of one another want a prefix that ends in the first. */
 int bsr_attend_prompt(bsr_ctx* ctx, const bsr_attn_args* args, void* stream);
 
 /* ---- instrumentation ----------------------------------------------------------- */

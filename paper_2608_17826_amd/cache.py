@@ -258,7 +258,9 @@ class PagedCache:
         """Attention of drafted trees, or of single tokens; ``tree``: int64 [tokens, words] masks.
 
         ``tensors``: the group's tensors that hold K and V, at ``offsets``
-        bytes of their records.  See bsr_attend_tree.
+        bytes of their records.  ``scale``: k_dim ** -0.5 by default; a model with
+        latent records scales by the width that its heads had before, not by 576,
+        and passes that.  See bsr_attend_tree.
         """
         _check(tree.dim() == 2 and 1 <= tree.shape[1] <= bsr.BSR_MAX_TREE_WORDS, "tree is [tokens, words]")
         return self._attend(bsr.bsr_attend_tree, group, tensors, q, batch, dims, kv_heads, max_len, offsets, scale,
@@ -270,7 +272,11 @@ class PagedCache:
                       prefix: Optional[torch.Tensor] = None, documents: Optional[torch.Tensor] = None,
                       out: Optional[torch.Tensor] = None, lse: bool = False):
         """Attention of prompt tokens, with a bias by distance (``slopes``, fp32 per head), bidirectional
-        prefixes (int32 per request) and packed documents (int32 first position per token).  See bsr_attend_prompt."""
+        prefixes (int32 per request) and packed documents (int32 first position per token).
+
+        A prefix that reaches past a row's document shows the row later ones' keys
+        too.  ``tensors``, ``offsets`` and ``scale`` as in :meth:`attend_tree`.  See bsr_attend_prompt.
+        """
         arrays = {"slopes": (slopes, torch.float32, q.shape[1]), "prefix": (prefix, torch.int32, batch.lens.numel()),
                   "documents": (documents, torch.int32, q.shape[0])}
         return self._attend(bsr.bsr_attend_prompt, group, tensors, q, batch, dims, kv_heads, max_len, offsets, scale,
