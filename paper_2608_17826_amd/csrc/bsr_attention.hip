@@ -1307,37 +1307,6 @@ hipError_t launch_typed(const AttnParams& p, hipStream_t s) {
 
 }  // namespace
 
-AttnTiling attn_tiling(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads, uint32_t n_kv_heads, uint32_t v_dim,
-                       uint32_t max_len) {
-  AttnTiling t{};
-  const uint32_t per_kv = n_heads / n_kv_heads;
-  t.tile_heads = per_kv < kTileRows ? per_kv : kTileRows;
-  t.tile_rows = kTileRows;
-  if (v_dim == 512 && n_requests && n_tokens && n_tokens % n_requests == 0) {
-    // requests of as many rows each, it seems (and at least one): no more row blocks
-    // than those need (16 rows over 128K: 52 us in a tile of 32, 69 in one of 128)
-    const uint64_t rows = static_cast<uint64_t>(n_tokens) / n_requests * t.tile_heads;
-    t.tile_rows = rows <= 32 ? 32 : rows <= 64 ? 64 : kTileRows;
-  }
-  t.tile_tokens = t.tile_rows / t.tile_heads;
-  t.units = n_kv_heads * ((per_kv + t.tile_heads - 1) / t.tile_heads);
-  // every request may end a tile early; none has a tile without a token
-  const uint64_t tiles = (n_tokens / t.tile_tokens) + static_cast<uint64_t>(n_requests < n_tokens ? n_requests : n_tokens);
-  t.base = t.items = tiles * t.units;
-  // two steps: one latent token over 1,000 keys takes 17.5 us, 20.7 with parts of 128
-  // at least; 20 tokens of heads of 128 14.6, 15.9 with 256, 15.2 with 64
-  t.min_part = v_dim == 512 ? 64 : 128;
-  if (max_len > t.min_part) {
-    t.target = v_dim == 512 ? 256 : v_dim == 128 ? 512 : kMaxTarget;  // workgroups that the GPU holds at once
-    const uint64_t parts = t.base <= t.target ? t.target : 2 * t.target;
-    const uint64_t most = t.base * ((max_len + t.min_part - 1) / t.min_part);
-    t.slots = most < parts ? most : parts;
-    if (t.items < t.slots) t.items = t.slots;
-    t.workspace = t.slots * t.tile_rows * (v_dim + 2) * sizeof(float);
-  }
-  return t;
-}
-
 hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
   return p.f16 ? launch_typed<_Float16>(p, s) : launch_typed<__bf16>(p, s);
 }
