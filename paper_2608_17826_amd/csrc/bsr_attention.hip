@@ -137,6 +137,12 @@ __device__ __forceinline__ uint32_t wave_sum(const AttnParams& p, uint32_t x) {
 //
 // One token of 64 heads (8 KV heads of 128) of 70 requests, 560 tiles: up to 20K
 // keys 571 us cut, 613 whole; up to 2K 81 and 78; up to 500 33.4 and 30.0.
+//
+// The rule goes by the batch's tiles and its sum, so one long range among many short
+// ones is cut the less the nearer the tiles come to target: such a token over
+// 131,072 keys among others over 1,000 takes 152 us of 32 requests, 252 of 48 and, whole,
+// 2,360 of 63 to 100 (the bytes 137 to 195); with latent records of 16 heads 105 us of 100
+// requests, 308 of 200, 6,300 of 255 and 300 (55 to 104).
 constexpr float kLongPart = 2048;  // keys
 __device__ __forceinline__ uint32_t part_keys(const AttnParams& p, const RequestWork& first) {
   constexpr uint32_t kWhole = 0x7fffffffu;
@@ -590,15 +596,23 @@ __device__ void redo_row(const AttnParams& p, const Request& q, const Work& w, c
 // rows meet in a bank (no conflict is counted).  Two buffers: step t + 1 is loaded,
 // past the registers, while t is computed.
 //
-// Heads of 128 leave registers for 2 workgroups a CU, heads of 64 for 3.  What
-// bounds it: with many rows the matrix and the vector unit in turn (a step's 32
-// products of a wave take 1,090 cycles, its 32 scores a lane some 900 without mask,
-// cap or bias), and the clock, 1.8 GHz under this load; with few rows the cache's
-// bytes.  1,024 tokens of 16 heads behind 128K: 1,100-1,170 us, 940-1,000
-// TFLOP/s; one token of 32 heads over 128K: 112 us, 4.8 TB/s; 8 trees of 64
-// nodes, 32 heads, capped, over 9,000: 52 us (the cap's exponential and reciprocal
-// are as many cycles as the rest of the softmax); 10.7K packed tokens of 16 heads
-// of 64 with a bias: 50 us (5.4 steps a tile, behind some 6 us to the first).
+// The weights are rounded to T for the products with V: products of fp32 run at a
+// sixteenth of the rate, and two halves of a weight would double the products.  It
+// costs at most 2^-8 (fp16 2^-11) of a row's sum of weight x |value|; measured, off from 64
+// bits by 0.0019-0.0024 for 0.0016-0.0017 with weights in fp32 (bf16, whose result alone is
+// rounded by as much), 2.7e-4 for 2.1e-4 (fp16).
+//
+// Heads of 128 leave registers for 2 workgroups a CU, heads of 64 for 3 (which with a
+// cap spill 15 to 21 registers).  What bounds it: with many rows the matrix and
+// the vector unit in turn (a step's 32 products of a wave take 1,090 cycles, its 32
+// scores a lane some 900 without mask, cap or bias), and the clock, 1.8 GHz under this
+// load; with few rows the cache's bytes; in between neither, but too few waves at
+// work: ramps, uneven tiles, waves without rows.  1,024 tokens of 16 heads behind
+// 128K: 1,110-1,170 us, 940-990 TFLOP/s (vector unit busy 55% of the time, matrix
+// unit 48%, 1.7 of 2 waves a SIMD); one token of 32 heads over 128K: 115 us with the
+// join, 4.7 TB/s; 8 trees of 64 nodes, 32 heads, capped, over 9,000: 52-54 us
+// (35%, 15%, 1.3 of 2); 10.7K packed tokens of 16 heads of 64 with a bias: 50 us (41%,
+// 11%, 1.5 of 3; 5.4 steps a tile, behind some 6 us to the first).
 // ---------------------------------------------------------------------------
 constexpr int kAttnThreads = 256;
 
@@ -831,9 +845,11 @@ __global__ __launch_bounds__(kAttnThreads, D == 64 ? 3 : 2) void k_attend_heads(
 // have a buffer more.  What bounds it: a step of 128 rows takes 5,000 cycles, of
 // which the products 2,310; a load holds its wave 80 cycles, 9 of them a step, and
 // the softmax of a step has only the products of the step before beside it.  4
-// nodes of 128 heads over 512K: 590-610 us, 960-990 TFLOP/s; 16 trees of 8 nodes, 16
-// heads, over up to 33K: 79 us, 3.3 TB/s; one token of 16 heads over 1,000: 12.3
-// us, of which 6 until the first records are there.
+// nodes of 128 heads over 512K: 607-615 us with the join, 950-960 TFLOP/s (vector unit busy
+// 22% of the time, matrix unit 41%); 16 trees of 8 nodes, 16 heads, over up to 33K: 79-82
+// us, 3.2-3.3 TB/s (18%, 24%, 0.76 of a wave a SIMD); one token of 16 heads over 1,000:
+// 12-13 us, of which 6 until the first records are there.  Tiles of 128 rows
+// spill 5 vector registers, 27 with cap and bias.
 // ---------------------------------------------------------------------------
 template <typename T, int kMods, int kBlocks>
 __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThreads, 1) void k_attend_latent(AttnParams p) {
@@ -1176,8 +1192,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(1, 1))) __launch_bounds__(kAttnThr
 // ---------------------------------------------------------------------------
 // Joins the parts of a row: sums and maxima as the running softmax would have
 // joined them, in an order that the sizes alone decide.  Bounded by the parts' bytes
-// and by finding the work: 512 parts of 128 rows of 128 (34 MB) 14 us, nothing to
-// join 4.5 us.
+// and by finding the work: 512 parts of 128 rows of 128 (34 MB) 14 us; 4.5 us
+// where the lengths, which the host does not know, leave nothing to join.
 // ---------------------------------------------------------------------------
 // Parts of a range, at most: of `target` for up to as many ranges, or of twice
 // that for more than `target` ranges, every other of which has a part too.

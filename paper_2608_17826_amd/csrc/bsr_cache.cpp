@@ -201,7 +201,8 @@ AttnTiling attn_tiling(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
   t.tile_rows = kTileRows;
   if (v_dim == 512 && n_requests && n_tokens && n_tokens % n_requests == 0) {
     // requests of as many rows each, it seems (and at least one): no more row blocks
-    // than those need (16 rows over 128K: 52 us in a tile of 32, 69 in one of 128)
+    // than those need (16 rows over 128K: 52 us in a tile of 32, 69 in one of 128).
+    // A padded row more, or rows that do not divide evenly, and all tiles have 128.
     const uint64_t rows = static_cast<uint64_t>(n_tokens) / n_requests * t.tile_heads;
     t.tile_rows = rows <= 32 ? 32 : rows <= 64 ? 64 : kTileRows;
   }

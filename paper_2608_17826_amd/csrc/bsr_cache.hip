@@ -61,9 +61,10 @@ __device__ __forceinline__ Lengths lengths_of(const TablesBuildParams& p, int32_
   return x;
 }
 
-// What bounds it is the way to memory and back, twice (the lengths, then the
-// block ids), 5 of the 6 us that 37 rows of four groups take; 268K rows (64
-// requests) take 8.7, with four rows a thread and a quarter of the workgroups 12.6.
+// What bounds it is the launch and three loads one behind the other (the lengths, a
+// row's request's own once more, out of the cache, and the block ids), 5 of the 6 us
+// that 37 rows of four groups take; 268K rows (64 requests) take 8.7, with four rows
+// a thread and a quarter of the workgroups 12.6.
 __global__ __launch_bounds__(kTablesThreads) void k_tables_build(TablesBuildParams p) {
   // [1 + n_groups][n_requests + 1]: rows, then blocks taken, before each request
   extern __shared__ uint32_t before[];
@@ -193,9 +194,10 @@ __device__ __forceinline__ bool append_unit(const AppendParams& p, uint64_t i, u
 
 // CONTIG records in units of eight values, from S to C (the same: copied bit by
 // bit).  Bounded by memory: 32,768 latent records of two sources (75.8 MB moved)
-// 12.9 us, 5.8 TB/s (part of the sources comes out of the caches); 64 records 2.9
-// us, the launch and two ways to memory.  One unit a thread: 13.8 and 2.2, and
-// where three inputs in turn stay in the caches 13.0 for 15.7.
+// 13.0 us, 5.8 TB/s (part of the sources comes out of the caches); 64 records 2.9
+// us, the launch and two ways to memory.  One unit a thread, in turn on one
+// box: 64 records the same, 8,192 of them 4.6 us for 6.0, 32,768 12.5-13.0 for
+// 13.0, and with inputs that stay in the caches 13.0 for 15.7.
 template <typename S, typename C>
 __global__ __launch_bounds__(kAppendThreads) void k_append(AppendParams p) {
   const uint64_t i0 = static_cast<uint64_t>(blockIdx.x) * (kAppendThreads * kAppendUnits) + threadIdx.x;
