@@ -120,24 +120,28 @@ class PagedCache:
         n_slots = sum(added) if n_slots is None else n_slots
         _check(sum(added) <= n_slots < 1 << 31, "n_slots is fewer than the new tokens, or not below 2^31")
         rows = [r for r in range(n) if added[r]]
-        take, back = [], []
-        for g in range(len(self.groups)):
-            have, held = {r: self.blocks(g, cached[r]) for r in rows}, self.held[g]
-            need = {r: self.blocks(g, cached[r] + added[r]) for r in rows}
-            for r in rows:
-                _check(have[r] <= held[r], f"group {g}: table row {r} holds {held[r]} blocks, fewer than {cached[r]} tokens")
-            take.append(sum(need.values()) - sum(have.values()))
-            back.append([(r, have[r], held[r]) for r in rows if have[r] < held[r]])
-            if max(need.values(), default=0) > self.tables[g].shape[1]:
+        at, to = [cached[r] for r in rows], [cached[r] + added[r] for r in rows]
+        take, back, then = [], [], []
+        for g, d in enumerate(self.groups):
+            B, held = d.block_tokens, [self.held[g][r] for r in rows]
+            have, need = [-(-t // B) for t in at], [-(-t // B) for t in to]
+            short = next((r for r, h, k in zip(rows, have, held) if h > k), None)
+            if short is not None:
+                raise bsr.BsrError(bsr.BSR_E_ARG, f"group {g}: table row {short} holds {self.held[g][short]} blocks, "
+                                   f"fewer than {cached[short]} tokens take")
+            if max(need, default=0) > self.tables[g].shape[1]:
                 raise bsr.BsrError(bsr.BSR_E_ARG, f"group {g}: a request outgrows its table")
-            left = self.free[g].numel() - self.taken[g] + sum(to - at for _, at, to in back[g])
+            take.append(sum(need) - sum(have))
+            left = self.free[g].numel() - self.taken[g] + sum(held) - sum(have)
             if take[g] > left:
                 raise bsr.BsrError(bsr.BSR_E_NOMEM, f"group {g}: {take[g]} blocks wanted, {left} free")
+            back.append([x for x in zip(rows, have, held) if x[1] < x[2]] if sum(held) > sum(have) else [])
+            then.append(need)
         for g, rests in enumerate(back):
             if rests:
-                self._give_back(g, [self.tables[g][r, at:to] for r, at, to in rests])
-                for r, at, _ in rests:
-                    self.held[g][r] = at
+                self._give_back(g, [self.tables[g][r, h:k] for r, h, k in rests])
+                for r, h, _ in rests:
+                    self.held[g][r] = h
         i32 = dict(dtype=torch.int32, device=self.device)
         lengths = torch.tensor([list(cached), list(added)], dtype=torch.int32, pin_memory=True).to(self.device, non_blocking=True)
         b = Batch(torch.empty(n + 1, **i32), torch.empty(n, **i32),
@@ -149,9 +153,9 @@ class PagedCache:
                                                        b.starts.data_ptr(), b.lens.data_ptr(), b.result.data_ptr()),
                              self._stream())
         self.taken = [t + k for t, k in zip(self.taken, take)]
-        for g, held in enumerate(self.held):
-            for r in rows:
-                held[r] = self.blocks(g, cached[r] + added[r])
+        for held, need in zip(self.held, then):
+            for r, k in zip(rows, need):
+                held[r] = k
         return b
 
     def release(self, row: int, tokens: int) -> None:
