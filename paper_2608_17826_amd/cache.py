@@ -264,7 +264,8 @@ class PagedCache:
         ``tensors``: the group's tensors that hold K and V, at ``offsets``
         bytes of their records.  ``scale``: k_dim ** -0.5 by default; a model with
         latent records scales by the width that its heads had before, not by 576,
-        and passes that.  See bsr_attend_tree.
+        and passes that.  Rows behind the batch's last are not written: of an output
+        that the call makes they hold anything.  See bsr_attend_tree.
         """
         _check(tree.dim() == 2 and 1 <= tree.shape[1] <= bsr.BSR_MAX_TREE_WORDS, "tree is [tokens, words]")
         return self._attend(bsr.bsr_attend_tree, group, tensors, q, batch, dims, kv_heads, max_len, offsets, scale,
